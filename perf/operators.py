@@ -337,7 +337,8 @@ def _bind(s):
         if op == "append":
             p.n_rows, p.ld_k, p.ld_v = s.n_rows, s.kv * s.D, s.kv * s.D
         else:
-            p.n_seqs, p.n_heads, p.max_q, p.max_len, p.table_width = s.B, s.heads, s.max_q, s.max_len, s.width
+            p.n_seqs, p.n_rows, p.n_heads, p.table_width = s.B, s.n_rows, s.heads, s.width
+            p.max_q, p.max_len = s.max_q, s.max_len
             p.ld_q = p.ld_out = s.heads * s.D
             p.scale = 1.0 / math.sqrt(s.D)
             p.workspace_bytes = ssd.ssd_kvq_workspace(c, p)
