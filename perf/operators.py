@@ -407,7 +407,8 @@ def _plain_append(s):
     slot = s.slots.long()
     page, off = slot // T, slot % T
     # the block that each request's first new row falls into holds older tokens before it
-    head = s.cu[:-1].long().clamp(max=max(s.n_rows - 1, 0))
+    # (a request without new rows repeats another's)
+    head = s.cu[s.seq[s.cu[:-1].long().clamp(max=s.n_rows - 1)]].long()
     hpage, hoff = page[head], off[head]
     token = torch.arange(T, device="cuda")
     for codes, exps, x, dim in ((s.k, s.ks, s.k_new, 2), (s.v, s.vs, s.v_new, 3)):  # keys [T][D], values [D][T]
