@@ -412,6 +412,197 @@ ssd_status ssd_decode_image_heads(ssd_model* model, const ssd_schedule* sched, i
                                   ssd_draft_head* const* v_heads, int32_t n_v, int32_t* out_tokens,
                                   ssd_stats* stats, void* stream);
 
+/*
+ * Serving operators.  What a server that decodes for many requests calls around
+ * its own projections, one decode or prefill step after the other: block tables
+ * and slot maps, rotary positions with several axes, a paged KV cache in 8 bits
+ * with the attention that reads it, and sampling.  They stand beside what the
+ * verify pass does inside (rotary factors of one axis, a contiguous bf16 cache,
+ * rules A to C) and need no model.
+ *
+ * Conventions of these calls (those of the library hold where nothing else is said):
+ *  - Arrays are device arrays of the current device, whole inside one allocation
+ *    and aligned to their elements; others, and a stream of another device, are
+ *    refused with SSD_E_INVAL before any launch.  An output may share memory
+ *    with another array of the call only where that is said.
+ *  - Work is enqueued on `stream` (a hipStream_t, NULL = default stream) and may
+ *    be captured into a graph.  Nothing is allocated, nothing synchronizes and
+ *    nothing is kept between calls.  Calls on different streams and threads are
+ *    independent as long as their arrays (workspaces among them) are.
+ *  - What the host cannot see (lengths, tables, slots) is bounds-checked by the
+ *    kernels: an entry that names no block or no row is skipped as each call says.
+ *  - SSD_E_DEVICE here poisons nothing: the arrays may hold part of a result.
+ */
+
+/*
+ * The cache of one layer, in memory of the caller: keys k [n_blocks][n_kv_heads][block]
+ * [head_dim] and values v [n_blocks][n_kv_heads][head_dim][block] as e4m3 codes (OCP: 1 sign,
+ * 4 exponent and 3 fraction bits, largest value 448), 16-byte aligned, and exponent bytes k_exp,
+ * v_exp [n_blocks][n_kv_heads]: a code of block p and head h stands for code * 2^(exp[p][h] - 127).
+ * block (tokens) is 16, 32, 64 or 128, head_dim 64 or 128; n_blocks * block < 2^31.
+ * A request's position p lies at offset p % block of the cache block that its
+ * block table names for p / block.  Memory need not be cleared: the exponent
+ * and the codes of a position are set when it is written, and what was never
+ * written must only not be inside a request's length.
+ */
+typedef struct {
+  void* k;
+  void* v;
+  uint8_t* k_exp;
+  uint8_t* v_exp;
+  int32_t n_blocks, block, n_kv_heads, head_dim;
+} ssd_kvq_cache;
+
+/*
+ * Block tables and slot maps from request lengths.  Request b of n_seqs holds
+ * held[b] tokens and gets fresh[b] more (negative counts as 0).  Blocks it lacks,
+ * ceil((held + fresh) / block) - ceil(held / block) of them (none past the table's
+ * width), come from pool [n_pool] (free block ids) in request order, from its front.
+ * table     [n_seqs][table_width] in/out: the entries of the blocks taken are
+ *           written, the others stay (those of held tokens are read).
+ * lens      [n_seqs] out: held + fresh.
+ * cu        [n_seqs + 1] out: running sum of fresh, cu[0] = 0: rows cu[b] ..
+ *           cu[b + 1] - 1 of a step's activations are request b's.
+ * slots     [n_rows] out: block id * block + offset of every new row, -1 for rows
+ *           behind the last request's, past the table's width, or without a block.
+ * positions [n_rows] out: the row's position in its request (-1 behind the last).
+ * used      [1] out: blocks asked of the pool.  More than n_pool: the pool was too
+ *           short, the entries it could not serve are -1.  The caller moves its
+ *           pool on by `used` and returns the blocks of finished requests.
+ * Calling it again with the same inputs gives the same outputs.
+ * Errors: SSD_E_INVAL for NULL arrays (pool may be NULL if n_pool = 0, slots and
+ * positions if n_rows = 0) and sizes: block as above, n_seqs >= 1,
+ * table_width >= 1, n_pool and n_rows >= 0.
+ */
+typedef struct {
+  int32_t n_seqs, block, table_width, n_pool, n_rows;
+} ssd_kvq_slot_params;
+ssd_status ssd_kvq_slots(const ssd_kvq_slot_params* params, const int32_t* held, const int32_t* fresh,
+                         const int32_t* pool, int32_t* table, int32_t* lens, int32_t* cu, int32_t* slots,
+                         int32_t* positions, int32_t* used, void* stream);
+
+/*
+ * Rotary positions with several axes (time, height and width of image and video
+ * tokens, for one): of each head's rotary pairs (j, j + half), half = the sum of
+ * section[0 .. n_axes), the first section[0] turn by the positions of axis 0, the
+ * next section[1] by those of axis 1, and so on:
+ *     angle = positions[axis][t] * theta^(-j / half),
+ *     (x_j, x_{j+half}) -> (x_j cos - x_{j+half} sin, x_{j+half} cos + x_j sin).
+ * Elements from 2 half on pass through.  One axis with section[0] = head_dim / 2 is
+ * the rotary embedding of the backbone (ssd_model_config); positions that are
+ * equal on all axes give the same.  Angles are formed in float64.
+ * q  [T][n_heads][head_dim], row t at q + t * ld_q elements; k the same with n_kv_heads
+ * and ld_k (so both may be columns of one projection's output); q_out, k_out likewise.
+ * An output may be its input (same address and ld); otherwise they must not overlap.
+ * positions int32 [n_axes][T], any value.  dtype SSD_F32 or SSD_BF16 (one rounding, of
+ * the result).
+ * Errors: SSD_E_INVAL for NULL arrays, T < 1, n_heads or n_kv_heads < 1, n_axes outside
+ * [1, 4], a negative section, half = 0, 2 half > head_dim, head_dim > 1024, a row
+ * length below its heads, theta not a finite number > 0.
+ */
+#define SSD_ROPE_AXES 4
+typedef struct {
+  int32_t n_heads, n_kv_heads, head_dim, dtype, n_axes;
+  int32_t section[SSD_ROPE_AXES];
+  int64_t ld_q, ld_k, ld_q_out, ld_k_out; /* elements */
+  double theta;
+} ssd_rope_params;
+ssd_status ssd_rope_axes(const ssd_rope_params* params, int32_t T, const void* q, const void* k,
+                         const int32_t* positions, void* q_out, void* k_out, void* stream);
+
+/*
+ * Write new keys and values: row r of k and v ([n_rows][n_kv_heads][head_dim], row r
+ * at r * ld elements; dtype SSD_F32 or SSD_BF16) to slot slots[r]; slots outside
+ * [0, n_blocks * block) are skipped.  The rows of one block must be consecutive
+ * rows with consecutive slots, one such run per block and call, and no row twice
+ * (what ssd_kvq_slots gives); runs may come in any order.
+ * A block's exponent (per head, keys and values apart) is the smallest, at least
+ * 1, whose scale takes the run's largest finite magnitude to at most 448.  A run
+ * that starts inside its block (offset > 0) appends to the tokens before it: the
+ * exponent is then at least the block's old one, and where it grows the older
+ * codes are rounded again to the new scale (exact unless they leave e4m3's normal
+ * range).  A run at offset 0 sets the exponent anew: what the block held is gone.
+ * Values are rounded to nearest, ties to even; infinities become the largest
+ * code, NaN becomes 0.  Codes behind the run stay as they were.
+ * Errors: SSD_E_INVAL for NULL arrays, a bad cache, n_rows < 0, a row length below
+ * n_kv_heads * head_dim, an unknown dtype.
+ */
+typedef struct {
+  int32_t dtype, n_rows;
+  int64_t ld_k, ld_v; /* elements */
+} ssd_kvq_append_params;
+ssd_status ssd_kvq_append(const ssd_kvq_cache* cache, const ssd_kvq_append_params* params, const int32_t* slots,
+                          const void* k, const void* v, void* stream);
+
+/*
+ * Causal attention of each request's newest rows over its cached positions, their
+ * own among them (append first): rows cu[b] .. cu[b + 1] - 1 of q sit at the last
+ * positions of request b, row i of its n at position lens[b] - n + i, and see the
+ * positions 0 .. that one (one row: an ordinary decode step; more: a verify round
+ * or a prompt).
+ *     out = softmax(scale * q k^T) v,   head h reads KV head h / (n_heads / n_kv_heads)
+ * q [n_rows][n_heads][head_dim] with row length ld_q (elements), out likewise with ld_out
+ * (may be q where ld_out = ld_q), dtype SSD_F32 or SSD_BF16; statistics and sums are
+ * fp32, the result is rounded once.  Rows that cu names outside [0, n_rows) are skipped.
+ * table [n_seqs][table_width]: entries outside [0, n_blocks) hide their positions; so
+ * do positions past the table's width.  A row that sees no position gets zeros.
+ * Rows of out that belong to no request stay as they were.
+ * max_q >= the most rows of a request (rows past it are not computed) and max_len
+ * >= the largest len (a hint that splits long contexts; a wrong one costs time only)
+ * are the host's bounds.  scale: any finite number (1/sqrt(head_dim) as a rule).
+ * workspace: ssd_kvq_workspace bytes (0: may be NULL), 16-byte aligned, for partial
+ * results; its contents do not matter before or after a call, but calls that run
+ * at the same time need one each (graphs that may overlap too).
+ * Errors: SSD_E_INVAL for NULL arrays, a bad cache, n_seqs, n_rows, max_q, max_len or
+ * table_width < 1, n_heads no multiple of n_kv_heads, a row length below n_heads *
+ * head_dim, an unknown dtype, a non-finite scale, too small a workspace.
+ */
+typedef struct {
+  int32_t dtype, n_seqs, n_rows, n_heads, max_q, max_len, table_width;
+  int64_t ld_q, ld_out; /* elements */
+  double scale;
+  int64_t workspace_bytes;
+} ssd_kvq_attn_params;
+/* bytes of workspace that a call with these sizes needs (-1: invalid; pointers are not looked at) */
+int64_t ssd_kvq_workspace(const ssd_kvq_cache* cache, const ssd_kvq_attn_params* params);
+ssd_status ssd_kvq_attention(const ssd_kvq_cache* cache, const ssd_kvq_attn_params* params, const void* q,
+                             const int32_t* cu, const int32_t* lens, const int32_t* table, void* out,
+                             void* workspace, void* stream);
+
+/*
+ * A code of every row of given logits (a session's carry or logits_out, say), from
+ * given uniforms:
+ *     w_v = exp((l_v - max l) / temperature), a distribution once divided by its sum;
+ *     top_k > 0 keeps the top_k largest (equal logits: lower ids first);
+ *     top_p < 1 keeps, of those in falling order (equal logits: lower ids first), the
+ *         shortest prefix that has top_p of their mass, at least one code;
+ *     min_p > 0 keeps those with w_v >= min_p (min_p times the largest probability);
+ *     the token is the smallest kept id whose running sum of w (id order) exceeds u
+ *         times the sum over all kept ids (u >= 1: the last kept id).
+ * temperature 0 takes the largest logit (lowest id).  -inf and NaN logits are never
+ * drawn, +inf counts as the largest finite number; a row without any other gives
+ * token -1 and probability 0.  Weights are float64, summed to 2^-46 of the largest
+ * (smaller ones count as 0): results do not depend on the order of any sum.
+ * logits [R][vocab] fp32, row r at r * ld; u [R] fp32; tokens [R] int32 out (ids count
+ * from 0); probs [R] fp32 out or NULL: the token's probability among those kept.
+ * temperatures, top_ks, top_ps, min_ps: NULL, or device arrays [R] (fp32, top_ks int32)
+ * in place of the number for all rows; there a temperature that is not > 0 takes
+ * the largest, and NaN for top_p or min_p switches it off.
+ * Errors: SSD_E_INVAL for NULL arrays, R < 1, vocab outside [1, 2^18], ld < vocab, and a
+ * temperature that is negative or not finite, or a NaN top_p or min_p, as numbers.
+ */
+typedef struct {
+  int32_t vocab, top_k; /* top_k <= 0: all */
+  int64_t ld;           /* elements */
+  double temperature, top_p, min_p;
+  const float* temperatures;
+  const int32_t* top_ks;
+  const float* top_ps;
+  const float* min_ps;
+} ssd_sample_params;
+ssd_status ssd_sample_logits(const ssd_sample_params* params, int32_t R, const float* logits, const float* u,
+                             int32_t* tokens, float* probs, void* stream);
+
 /* Thread-local description of the last error (empty string if none). */
 const char* ssd_last_error(void);
 

@@ -22,6 +22,7 @@ EXPORTED = [
     "ssd_verify_step", "ssd_get_carry", "ssd_session_set_cfg", "ssd_decode_image", "ssd_profile", "ssd_profile_read", "ssd_last_error",
     "ssd_draft_head_numel", "ssd_draft_head_init", "ssd_draft_head_run", "ssd_free_draft_head",
     "ssd_decode_image_heads", "ssd_plant_image", "ssd_draft_head_run_noalloc",
+    "ssd_kvq_slots", "ssd_rope_axes", "ssd_kvq_append", "ssd_kvq_workspace", "ssd_kvq_attention", "ssd_sample_logits",
 ]
 
 
@@ -57,6 +58,45 @@ class ssd_stats(ctypes.Structure):
     _fields_ = [("passes", ctypes.c_int64), ("verify_rounds", ctypes.c_int64), ("accepted", ctypes.c_int64),
                 ("proposed", ctypes.c_int64), ("accepted_round", ctypes.c_int64 * 8),
                 ("proposed_round", ctypes.c_int64 * 8), ("wall_ns", ctypes.c_int64)]
+
+
+SSD_ROPE_AXES = 4
+
+
+class ssd_kvq_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_exp", ctypes.c_void_p), ("v_exp", ctypes.c_void_p),
+                ("n_blocks", ctypes.c_int32), ("block", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32)]
+
+
+class ssd_kvq_slot_params(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("block", ctypes.c_int32), ("table_width", ctypes.c_int32),
+                ("n_pool", ctypes.c_int32), ("n_rows", ctypes.c_int32)]
+
+
+class ssd_rope_params(ctypes.Structure):
+    _fields_ = [("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("n_axes", ctypes.c_int32), ("section", ctypes.c_int32 * SSD_ROPE_AXES),
+                ("ld_q", ctypes.c_int64), ("ld_k", ctypes.c_int64), ("ld_q_out", ctypes.c_int64),
+                ("ld_k_out", ctypes.c_int64), ("theta", ctypes.c_double)]
+
+
+class ssd_kvq_append_params(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("n_rows", ctypes.c_int32), ("ld_k", ctypes.c_int64), ("ld_v", ctypes.c_int64)]
+
+
+class ssd_kvq_attn_params(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("n_seqs", ctypes.c_int32), ("n_rows", ctypes.c_int32),
+                ("n_heads", ctypes.c_int32), ("max_q", ctypes.c_int32), ("max_len", ctypes.c_int32),
+                ("table_width", ctypes.c_int32), ("ld_q", ctypes.c_int64), ("ld_out", ctypes.c_int64),
+                ("scale", ctypes.c_double), ("workspace_bytes", ctypes.c_int64)]
+
+
+class ssd_sample_params(ctypes.Structure):
+    _fields_ = [("vocab", ctypes.c_int32), ("top_k", ctypes.c_int32), ("ld", ctypes.c_int64),
+                ("temperature", ctypes.c_double), ("top_p", ctypes.c_double), ("min_p", ctypes.c_double),
+                ("temperatures", ctypes.c_void_p), ("top_ks", ctypes.c_void_p), ("top_ps", ctypes.c_void_p),
+                ("min_ps", ctypes.c_void_p)]
 
 
 _lib = None
@@ -98,6 +138,15 @@ def lib():
         L.ssd_free_draft_head.restype = None
         L.ssd_last_error.argtypes = []
         L.ssd_last_error.restype = ctypes.c_char_p
+        L.ssd_kvq_slots.argtypes = [ctypes.POINTER(ssd_kvq_slot_params)] + [vp] * 10
+        L.ssd_rope_axes.argtypes = [ctypes.POINTER(ssd_rope_params), i32] + [vp] * 6
+        L.ssd_kvq_append.argtypes = [ctypes.POINTER(ssd_kvq_cache), ctypes.POINTER(ssd_kvq_append_params)] + [vp] * 4
+        L.ssd_kvq_workspace.argtypes = [ctypes.POINTER(ssd_kvq_cache), ctypes.POINTER(ssd_kvq_attn_params)]
+        L.ssd_kvq_workspace.restype = i64
+        L.ssd_kvq_attention.argtypes = [ctypes.POINTER(ssd_kvq_cache), ctypes.POINTER(ssd_kvq_attn_params)] + [vp] * 7
+        L.ssd_sample_logits.argtypes = [ctypes.POINTER(ssd_sample_params), i32] + [vp] * 5
+        for name in ("ssd_kvq_slots", "ssd_rope_axes", "ssd_kvq_append", "ssd_kvq_attention", "ssd_sample_logits"):
+            getattr(L, name).restype = i32
         for name in ("ssd_init_model", "ssd_prefill", "ssd_verify_step", "ssd_get_carry", "ssd_session_set_cfg",
                      "ssd_decode_image", "ssd_profile", "ssd_profile_read", "ssd_draft_head_init", "ssd_draft_head_run",
                      "ssd_decode_image_heads", "ssd_plant_image", "ssd_draft_head_run_noalloc"):
@@ -219,6 +268,40 @@ def ssd_decode_image_heads(model, sched, B, P, prefix, h_heads, v_heads, out_tok
                                         len(h_heads), vh, len(v_heads), _ptr(out_tokens), ctypes.byref(st),
                                         _ptr(stream)))
     return st
+
+
+def ssd_kvq_slots(params, held, fresh, pool, table, lens, cu, slots, positions, used, stream=None):
+    """Block tables (in place), lens, cu, slots, positions and used from request lengths; all int32 device arrays."""
+    _check(lib().ssd_kvq_slots(ctypes.byref(params), _ptr(held), _ptr(fresh), _ptr(pool), _ptr(table), _ptr(lens),
+                               _ptr(cu), _ptr(slots), _ptr(positions), _ptr(used), _ptr(stream)))
+
+
+def ssd_rope_axes(params, T, q, k, positions, q_out, k_out, stream=None):
+    """Rotates T rows of q and k by their positions [n_axes][T]; strided rows are given by address and params.ld_*."""
+    _check(lib().ssd_rope_axes(ctypes.byref(params), T, _ptr(q), _ptr(k), _ptr(positions), _ptr(q_out), _ptr(k_out),
+                               _ptr(stream)))
+
+
+def ssd_kvq_append(cache, params, slots, k, v, stream=None):
+    _check(lib().ssd_kvq_append(ctypes.byref(cache), ctypes.byref(params), _ptr(slots), _ptr(k), _ptr(v), _ptr(stream)))
+
+
+def ssd_kvq_workspace(cache, params):
+    """Bytes of workspace of a ssd_kvq_attention call with these sizes."""
+    n = int(lib().ssd_kvq_workspace(ctypes.byref(cache), ctypes.byref(params)))
+    if n < 0:
+        raise SSDError(SSD_E_INVAL, ssd_last_error())
+    return n
+
+
+def ssd_kvq_attention(cache, params, q, cu, lens, table, out, workspace=None, stream=None):
+    _check(lib().ssd_kvq_attention(ctypes.byref(cache), ctypes.byref(params), _ptr(q), _ptr(cu), _ptr(lens), _ptr(table),
+                                   _ptr(out), _ptr(workspace), _ptr(stream)))
+
+
+def ssd_sample_logits(params, R, logits, u, tokens, probs=None, stream=None):
+    _check(lib().ssd_sample_logits(ctypes.byref(params), R, _ptr(logits), _ptr(u), _ptr(tokens), _ptr(probs),
+                                   _ptr(stream)))
 
 
 def ssd_profile(model, enable):

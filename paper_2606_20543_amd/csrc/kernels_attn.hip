@@ -22,6 +22,7 @@
 // run on workgroups of one XCD, and the last to arrive combines them in chunk
 // order.
 #include "tiles.h"
+#include "kvq.h"
 
 namespace ssd {
 

@@ -1050,3 +1050,6 @@ void add_i32(int* p, int n, int delta, hipStream_t st) {
 }
 
 }  // namespace ssd
+
+#include "sample.h"
+#include "serve.h"

@@ -1,0 +1,192 @@
+// Serving operators that stand beside the verify pass: block tables and slot
+// maps from request lengths, and rotary positions with several axes
+// (device code and launchers, included by kernels_misc.hip).
+#pragma once
+
+#include "ssd_internal.h"
+
+namespace ssd {
+
+// ---------------- block tables and slot maps ----------------
+// Request b holds held_b tokens and gets fresh_b more.  With T tokens a block it has
+// ceil(held / T) blocks and needs ceil((held + fresh) / T); the blocks that the
+// requests lack come from the pool in request order, so the first of request b
+// is pool[sum of the lacks before b].  A workgroup owns SLOT_SEQS requests and
+// sums the lengths of all requests before them itself (a few loads a thread),
+// so one launch does it with no hand-off between workgroups.  Bound by its
+// launch and three dependent round trips (lengths, table or pool entry, store).
+constexpr int SLOT_T = 256, SLOT_SEQS = 8;
+
+__device__ __forceinline__ long long wave_sum_ll(long long v) {
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+
+// blocks of n tokens, at most the table's width
+__device__ __forceinline__ int slot_blocks(long long n, int T, int width) {
+  const long long c = (n + T - 1) / T;
+  return (int)(c < width ? c : width);
+}
+
+__global__ __launch_bounds__(SLOT_T) void slots_kernel(SlotArgs a) {
+  __shared__ long long red[2][SLOT_T / 64];
+  __shared__ int s_held[SLOT_SEQS], s_have[SLOT_SEQS];
+  __shared__ long long s_start[SLOT_SEQS + 1], s_cu[SLOT_SEQS + 1];
+  const int tid = threadIdx.x, b0 = blockIdx.x * SLOT_SEQS, nb = min(SLOT_SEQS, a.B - b0);
+  const int T = a.T, W = a.width;
+  // rows and lacking blocks of the requests before this workgroup's
+  long long rows = 0, lack = 0;
+  for (int b = tid; b < b0; b += SLOT_T) {
+    const long long h = max(a.held[b], 0), n = max(a.fresh[b], 0);
+    rows += n;
+    lack += slot_blocks(h + n, T, W) - slot_blocks(h, T, W);
+  }
+  rows = wave_sum_ll(rows);
+  lack = wave_sum_ll(lack);
+  if ((tid & 63) == 0) {
+    red[0][tid >> 6] = rows;
+    red[1][tid >> 6] = lack;
+  }
+  __syncthreads();
+  if (tid == 0) {
+    long long r = 0, l = 0;
+    for (int w = 0; w < SLOT_T / 64; ++w) {
+      r += red[0][w];
+      l += red[1][w];
+    }
+    if (b0 == 0) a.cu[0] = 0;
+    for (int i = 0; i < nb; ++i) {
+      const long long h = max(a.held[b0 + i], 0), n = max(a.fresh[b0 + i], 0);
+      s_held[i] = (int)h;
+      s_have[i] = slot_blocks(h, T, W);
+      s_cu[i] = r;
+      s_start[i] = l;
+      r += n;
+      l += slot_blocks(h + n, T, W) - s_have[i];
+      a.cu[b0 + i + 1] = (int)(r < INT_MAX ? r : INT_MAX);
+      a.lens[b0 + i] = (int)(h + n < INT_MAX ? h + n : INT_MAX);
+    }
+    s_cu[nb] = r;
+    s_start[nb] = l;
+    if (b0 + nb == a.B) a.used[0] = (int)(l < INT_MAX ? l : INT_MAX);
+  }
+  __syncthreads();
+  // table entries of the blocks taken here (an empty pool leaves -1)
+  auto pooled = [&](long long i) { return i < a.n_pool ? a.pool[i] : -1; };
+  for (long long e = s_start[0] + tid; e < s_start[nb]; e += SLOT_T) {
+    int i = 0;
+    while (s_start[i + 1] <= e) ++i;
+    a.table[(size_t)(b0 + i) * W + s_have[i] + (e - s_start[i])] = pooled(e);
+  }
+  // new rows, and behind the last request the padding
+  const long long last = b0 + nb == a.B ? a.n_rows : min(s_cu[nb], (long long)a.n_rows);
+  for (long long r = s_cu[0] + tid; r < last; r += SLOT_T) {
+    int slot = -1, pos = -1;
+    if (r < s_cu[nb]) {
+      int i = 0;
+      while (s_cu[i + 1] <= r) ++i;
+      const long long p = s_held[i] + (r - s_cu[i]);
+      const long long j = p / T;
+      pos = (int)(p < INT_MAX ? p : INT_MAX);
+      if (j < W) {
+        const int page = j >= s_have[i] ? pooled(s_start[i] + (j - s_have[i])) : a.table[(size_t)(b0 + i) * W + j];
+        const long long at = (long long)page * T + p % T;
+        if (page >= 0 && at <= INT_MAX) slot = (int)at;
+      }
+    }
+    a.slots[r] = slot;
+    a.positions[r] = pos;
+  }
+}
+
+void kvq_slots(const SlotArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL(slots_kernel, dim3((a.B + SLOT_SEQS - 1) / SLOT_SEQS), dim3(SLOT_T), 0, st, a);
+}
+
+// ---------------- rotary positions with several axes ----------------
+// Pair j (elements j and j + half) of every head turns by
+// pos[axis of j][t] * theta^(-j / half).  The angle is formed in float64 and
+// reduced to a part of a half turn there, so far positions keep their phase;
+// its remainder below the fp32 value enters to first order.  A workgroup makes
+// the factors of its tokens' pairs once, in LDS, for all heads.  Bound by HBM
+// at many tokens (each element read and written once).
+constexpr int ROPE_T = 256;
+
+template <typename E, int N>
+struct alignas(sizeof(E) * N) RopeVec {
+  E v[N];
+};
+__device__ __forceinline__ float rope_ld(float x) { return x; }
+__device__ __forceinline__ float rope_ld(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+__device__ __forceinline__ void rope_st(float& d, float x) { d = x; }
+// one rounding to bf16, of the finished value (NaN kept: the carry of the rounding must not make it infinite)
+__device__ __forceinline__ void rope_st(uint16_t& d, float x) {
+  const uint32_t u = __float_as_uint(x);
+  d = x == x ? (uint16_t)((u + 0x7FFFu + ((u >> 16) & 1u)) >> 16) : (uint16_t)((u >> 16) | 0x40u);
+}
+
+template <typename E, int N>
+__global__ __launch_bounds__(ROPE_T) void rope_axes_kernel(RopeArgs a, int TB) {
+  extern __shared__ float2 fac[];  // [TB][half]
+  const int tid = threadIdx.x, half = a.half, t0 = blockIdx.x * TB, nt = min(TB, a.T - t0);
+  for (int i = tid; i < nt * half; i += ROPE_T) {
+    const int t = i / half, j = i - t * half;
+    int ax = 0, end = a.section[0];
+    while (j >= end) end += a.section[++ax];
+    // angle / pi, less whole turns: in [-1, 1]
+    const double turn = (double)a.pos[(size_t)ax * a.T + t0 + t] * (exp2(-(double)j / half * a.log2_theta) * 0.15915494309189535);
+    const double x = 2.0 * (turn - rint(turn));
+    const float xh = (float)x;
+    const float d = (float)(x - (double)xh) * 3.14159265f;
+    float s, c;
+    sincospif(xh, &s, &c);
+    fac[i] = make_float2(fmaf(-s, d, c), fmaf(c, d, s));
+  }
+  __syncthreads();
+  const int pairs = half / N, rest = (a.D - 2 * half) / N, per = pairs + rest, heads = a.Hq + a.Hkv;
+  typedef RopeVec<E, N> V;
+  for (int i = tid; i < nt * heads * per; i += ROPE_T) {
+    const int t = i / (heads * per), r = i - t * heads * per, h = r / per, c = r - h * per;
+    const size_t tok = t0 + t;
+    const E* src = h < a.Hq ? (const E*)a.q + tok * a.ld_q + (size_t)h * a.D
+                            : (const E*)a.k + tok * a.ld_k + (size_t)(h - a.Hq) * a.D;
+    E* dst = h < a.Hq ? (E*)a.qo + tok * a.ld_qo + (size_t)h * a.D
+                      : (E*)a.ko + tok * a.ld_ko + (size_t)(h - a.Hq) * a.D;
+    if (c < pairs) {
+      const V x = *(const V*)(src + c * N), y = *(const V*)(src + half + c * N);
+      V u, w;
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float2 f = fac[t * half + c * N + e];
+        const float p = rope_ld(x.v[e]), q = rope_ld(y.v[e]);
+        rope_st(u.v[e], p * f.x - q * f.y);
+        rope_st(w.v[e], q * f.x + p * f.y);
+      }
+      *(V*)(dst + c * N) = u;
+      *(V*)(dst + half + c * N) = w;
+    } else {
+      const int o = 2 * half + (c - pairs) * N;
+      *(V*)(dst + o) = *(const V*)(src + o);
+    }
+  }
+}
+
+void rope_axes(const RopeArgs& a, hipStream_t st) {
+  const int TB = std::max(1, std::min(4, 1024 / a.half));
+  const dim3 grid((a.T + TB - 1) / TB);
+  const size_t lds = (size_t)TB * a.half * sizeof(float2);
+  // 16-byte accesses where every row, head and half starts on one
+  const int N = a.bf16 ? 8 : 4;
+  const uintptr_t at = (uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.qo | (uintptr_t)a.ko;
+  const bool vec = at % 16 == 0 && a.half % N == 0 && a.D % N == 0 &&
+                   (a.ld_q | a.ld_k | a.ld_qo | a.ld_ko) % N == 0;
+  if (a.bf16) {
+    if (vec) hipLaunchKernelGGL((rope_axes_kernel<uint16_t, 8>), grid, dim3(ROPE_T), lds, st, a, TB);
+    else hipLaunchKernelGGL((rope_axes_kernel<uint16_t, 1>), grid, dim3(ROPE_T), lds, st, a, TB);
+  } else {
+    if (vec) hipLaunchKernelGGL((rope_axes_kernel<float, 4>), grid, dim3(ROPE_T), lds, st, a, TB);
+    else hipLaunchKernelGGL((rope_axes_kernel<float, 1>), grid, dim3(ROPE_T), lds, st, a, TB);
+  }
+}
+
+}  // namespace ssd

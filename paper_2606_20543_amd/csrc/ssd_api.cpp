@@ -2816,3 +2816,5 @@ ssd_status ssd_decode_image_heads(ssd_model* m, const ssd_schedule* sc, int32_t 
 }
 
 }  // extern "C"
+
+#include "serve_api.h"

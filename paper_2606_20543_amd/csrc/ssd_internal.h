@@ -34,6 +34,7 @@
 
 #include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
+#include <limits.h>
 #include <stdint.h>
 
 #include <vector>
@@ -436,6 +437,56 @@ void gather_block(const int* img, int img_stride, const int* f, int P, int K, in
 void add_i32(int* p, int n, int delta, hipStream_t st);
 // rotary factors (cos, sin) of position p and pair j at tab[p * half + j]
 void rope_table(float2* tab, int positions, int half, double theta, hipStream_t st);
+// ---- serving operators (serve.h, sample.h, kvq.h; the ssd_kvq_*, ssd_rope_axes and ssd_sample_logits entry points) ----
+struct SlotArgs {
+  int B, T, width, n_pool, n_rows;
+  const int *held, *fresh, *pool;
+  int *table, *lens, *cu, *slots, *positions, *used;
+};
+void kvq_slots(const SlotArgs& a, hipStream_t st);
+struct RopeArgs {
+  int T, Hq, Hkv, D, half, bf16;
+  int section[SSD_ROPE_AXES];
+  double log2_theta;
+  size_t ld_q, ld_k, ld_qo, ld_ko;
+  const void *q, *k;
+  void *qo, *ko;
+  const int* pos;  // [axes][T]
+};
+void rope_axes(const RopeArgs& a, hipStream_t st);
+struct SampleArgs {
+  int R, V, top_k;
+  size_t ld;
+  double temperature, top_p, min_p;
+  const float *temperatures, *top_ps, *min_ps;  // [R], or nullptr: the number for all rows
+  const int* top_ks;
+  const float *logits, *u;
+  int* tokens;
+  float* probs;  // or nullptr
+};
+void sample_logits(const SampleArgs& a, hipStream_t st);
+struct KvqAppendArgs {
+  uint8_t *kc, *vc, *ke, *ve;
+  int n_blocks, T, Hkv, D, n_rows, bf16;
+  const int* slots;
+  const void *k, *v;
+  size_t ld_k, ld_v;
+};
+void kvq_append(const KvqAppendArgs& a, hipStream_t st);
+struct KvqAttnArgs {
+  const uint8_t *kc, *vc, *ke, *ve;
+  int n_blocks, T, Hkv, D;
+  int B, n_rows, Hq, max_q, max_len, width, bf16;
+  const void* q;
+  void* o;
+  size_t ld_q, ld_o;
+  const int *cu, *lens, *table;
+  float scale;
+  void* workspace;
+};
+size_t kvq_attn_workspace(const KvqAttnArgs& a);  // bytes
+void kvq_attention(const KvqAttnArgs& a, hipStream_t st);
+
 // fill helpers (graph-capture safe)
 void fill_u32(unsigned* p, size_t n, unsigned v, hipStream_t st);
 // out[w] = XCD index workgroup w ran on
