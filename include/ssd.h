@@ -555,7 +555,8 @@ ssd_status ssd_kvq_append(const ssd_kvq_cache* cache, const ssd_kvq_append_param
  * at the same time need one each (graphs that may overlap too).
  * Errors: SSD_E_INVAL for NULL arrays, a bad cache, n_seqs, n_rows, max_q, max_len or
  * table_width < 1, n_heads no multiple of n_kv_heads, a row length below n_heads *
- * head_dim, an unknown dtype, a non-finite scale, too small a workspace.
+ * head_dim, an unknown dtype, a non-finite scale, too small a workspace,
+ * n_seqs * max_q * n_heads of 2^31 or more, a table of more than 2^30 positions.
  */
 typedef struct {
   int32_t dtype, n_seqs, n_rows, n_heads, max_q, max_len, table_width;

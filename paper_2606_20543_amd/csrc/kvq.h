@@ -62,6 +62,18 @@ __device__ __forceinline__ float kvq_ld<float>(const float* p) { return *p; }
 template <>
 __device__ __forceinline__ float kvq_ld<uint16_t>(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
 
+// o / l as four elements of the output, zeros where no key was seen
+__device__ __forceinline__ void kvq_store4(float* p, floatx4 o, float l) {
+  const float f = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) p[e] = o[e] * f;
+}
+__device__ __forceinline__ void kvq_store4(uint16_t* p, floatx4 o, float l) {
+  const float f = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) p[e] = f2bf(o[e] * f);
+}
+
 template <typename E>
 __global__ __launch_bounds__(256) void kvq_append_kernel(KvqAppendArgs a) {
   const int lane = threadIdx.x & 63;
@@ -129,79 +141,462 @@ void kvq_append(const KvqAppendArgs& a, hipStream_t st) {
 // position whose table entry is no block of the cache is seen by none; a row
 // that sees nothing gets zeros.
 //
-// Plain kernel: a workgroup for each row and query head, a running maximum and
-// sum over tiles of 256 keys; a thread scores one key, then sums one dim over
-// its share of the tile.
-template <typename E>
-__global__ __launch_bounds__(256) void kvq_attn_kernel(KvqAttnArgs a) {
-  __shared__ float qs[128], ps[256], red[4], part[256];
-  const int tid = threadIdx.x, b = blockIdx.x / a.max_q, i = blockIdx.x - b * a.max_q, hq = blockIdx.y;
-  const int D = a.D, T = a.T, h = hq / (a.Hq / a.Hkv);
-  const int r0 = a.cu[b];
-  const long long n = (long long)a.cu[b + 1] - r0, row = (long long)r0 + i;
-  if (i >= n || row < 0 || row >= a.n_rows) return;
-  const int seen = (int)min((long long)a.width * T, (long long)a.lens[b] - n + i + 1);  // keys of this row (none: <= 0)
-  if (tid < D) qs[tid] = kvq_ld((const E*)a.q + row * a.ld_q + (size_t)hq * D + tid);
-  const int d = tid % D, np = 256 / D, pt = tid / D;
-  float m = -INFINITY, l = 0.f, acc = 0.f;
-  for (int j0 = 0; j0 < seen; j0 += 256) {
-    __syncthreads();
-    const int j = j0 + tid;
-    float s = -INFINITY;
-    if (j < seen) {
-      const int page = a.table[(size_t)b * a.width + j / T];
-      if (page >= 0 && page < a.n_blocks) {
-        const uint32_t* kp = (const uint32_t*)(a.kc + (((size_t)page * a.Hkv + h) * T + j % T) * D);
-        float x = 0.f;
-        for (int c = 0; c < D / 4; ++c) {
-          float v[4];
-          kvq_value4(kp[c], v);
-          for (int e = 0; e < 4; ++e) x = fmaf(v[e], qs[c * 4 + e], x);
-        }
-        s = x * kvq_pow2((int)a.ke[(size_t)page * a.Hkv + h] - 127) * a.scale;
-      }
-    }
-    float mt = s;
-    for (int o = 32; o > 0; o >>= 1) mt = fmaxf(mt, __shfl_xor(mt, o));
-    if ((tid & 63) == 0) red[tid >> 6] = mt;
-    __syncthreads();
-    mt = fmaxf(m, fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])));
-    const float f = m == mt ? 1.f : expf(m - mt);  // (nothing seen so far: exp(-inf) = 0)
-    const float p = s == -INFINITY ? 0.f : expf(s - mt);
-    m = mt;
-    ps[tid] = p;
-    float lt = p;
-    for (int o = 32; o > 0; o >>= 1) lt += __shfl_xor(lt, o);
-    __syncthreads();
-    if ((tid & 63) == 0) red[tid >> 6] = lt;
-    __syncthreads();
-    l = l * f + ((red[0] + red[1]) + (red[2] + red[3]));
-    acc *= f;
-    for (int t = pt; t < 256 && j0 + t < seen; t += np) {
-      const int page = a.table[(size_t)b * a.width + (j0 + t) / T];
-      if (page < 0 || page >= a.n_blocks) continue;
-      const size_t head = (size_t)page * a.Hkv + h;
-      const float v = __builtin_amdgcn_cvt_f32_fp8((int)a.vc[(head * D + d) * T + (j0 + t) % T], 0);
-      acc = fmaf(ps[t], v * kvq_pow2((int)a.ve[head] - 127), acc);
+// The rows of a request that share a KV head (i * g + head in group, g = query heads
+// a KV head) are the columns of 16-wide matrix products, S^T = K Q^T and O^T = V^T P^T,
+// over steps of 64 keys, with a running maximum and sum.  Key 16 G + 4 t + i of a
+// step is row 4 G + i of the t-th 16 x 16 tile of S^T, so lane group G (16 lanes)
+// holds the weights of 16 consecutive keys of each query: these are the operand
+// of the second product without a move, its V^T operand is 16 consecutive bytes of
+// the value layout, and since blocks have at least 16 tokens all of them share
+// one table entry and one scale.
+//
+// Keys are converted to bf16 with their scale (exact); bf16 queries are one
+// operand, fp32 ones the sum of three (all 24 bits).  Weights are p = 2^(t - m) in fp32,
+// t the score in the log2 domain.  fp32 calls split them into three bf16 operands like
+// the queries, the values being bf16 with their scale.  bf16 calls have one operand:
+// the weights take the value scale along, p' = 2^(t + e - R), e the value exponent of the
+// key's block and R a running bound of t + e, so that the codes themselves, exact in fp16,
+// are the other operand whatever the scales of different blocks are; p' is rounded to fp16,
+// 11 bits where the output has 8.  m and R follow their maxima lazily: the
+// sums are rescaled only where one has grown by more than 2^8.
+typedef _Float16 kvq_h8 __attribute__((ext_vector_type(8)));
+typedef _Float16 kvq_h2 __attribute__((ext_vector_type(2)));
+
+constexpr int KVQ_STEP = 64;
+constexpr float KVQ_NONE = -1e30f;  // m and R before the first key
+constexpr float KVQ_LAZY = 8.f;
+constexpr float KVQ_LIFT = 6.f;     // p' of the largest lies at 2^6 (2^14 before R moves on): fp16 steps of 2^-30 of it
+
+template <int D>
+struct KvqStage {
+  uint4 k[4][D / 64];  // 16 codes of key (tile t, row lane % 16), dims 64 u + 16 (lane / 16) ..
+  uint4 v[D / 16];     // 16 keys of dim 16 dt + lane % 16
+  int ek, ev;          // exponents: of this lane's key rows, of its 16 keys (-1: not in the cache)
+};
+
+// where a lane's 16 keys of a step lie
+struct KvqPlace {
+  int k, v;  // blocks of the key rows' group and of the value group; -1: none
+};
+
+template <int D>
+struct KvqWalk {
+  const KvqAttnArgs& a;
+  const int* trow;
+  int h, lane, kend, sh;  // sh: log2 of the block size
+  size_t blk;             // bytes of one block of one side
+  __device__ __forceinline__ KvqWalk(const KvqAttnArgs& args, int b, int head, int end)
+      : a(args), trow(args.table + (size_t)b * args.width), h(head), lane(threadIdx.x & 63), kend(end),
+        sh(__builtin_ctz(args.T)), blk((size_t)args.Hkv * args.T * D) {}
+  __device__ __forceinline__ int entry(int key) const {
+    const int p = trow[min(key >> sh, a.width - 1)];
+    return key < kend && (unsigned)p < (unsigned)a.n_blocks ? p : -1;
+  }
+  __device__ __forceinline__ KvqPlace place(int j0) const {
+    return KvqPlace{entry(j0 + 16 * ((lane & 15) >> 2)), entry(j0 + 16 * (lane >> 4))};
+  }
+  // (a missing block loads block 0 in its place, unused)
+  __device__ __forceinline__ void load(KvqStage<D>& s, int j0, const KvqPlace& pl) const {
+    const int m = lane & 15, c = lane >> 4, T = a.T;
+    const int pk = max(pl.k, 0), pv = max(pl.v, 0);
+    const uint8_t* kb = a.kc + (size_t)pk * blk + (size_t)(h * T + ((j0 + 16 * (m >> 2)) & (T - 1)) + (m & 3)) * D + 16 * c;
+    const uint8_t* vb = a.vc + (size_t)pv * blk + (size_t)(h * D + m) * T + ((j0 + 16 * c) & (T - 1));
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int u = 0; u < D / 64; ++u) s.k[t][u] = *(const uint4*)(kb + 4 * t * D + 64 * u);
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) s.v[dt] = *(const uint4*)(vb + (size_t)(16 * dt) * T);
+    s.ek = a.ke[(size_t)pk * a.Hkv + h];
+    s.ev = a.ve[(size_t)pv * a.Hkv + h];
+    if (pl.k < 0) s.ek = 127;
+    if (pl.v < 0) s.ev = -1;
+  }
+};
+
+__device__ __forceinline__ bf16x8 kvq_bf16x8(uint32_t lo, uint32_t hi, float scale) {
+  bf16x8 r;
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false),
+               b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true),
+               c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false),
+               d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+  r[0] = a[0], r[1] = a[1], r[2] = b[0], r[3] = b[1], r[4] = c[0], r[5] = c[1], r[6] = d[0], r[7] = d[1];
+  return r;
+}
+__device__ __forceinline__ kvq_h8 kvq_f16x8(uint32_t lo, uint32_t hi) {
+  kvq_h8 r;
+  const kvq_h2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true),
+               c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true);
+  r[0] = a[0], r[1] = a[1], r[2] = b[0], r[3] = b[1], r[4] = c[0], r[5] = c[1], r[6] = d[0], r[7] = d[1];
+  return r;
+}
+
+// largest over the four lane groups, in every lane
+__device__ __forceinline__ float kvq_max_groups(float x) {
+  x = fmaxf(x, __shfl_xor(x, 16));
+  return fmaxf(x, __shfl_xor(x, 32));
+}
+
+// Running state of QT tiles of 16 query rows in one wave; PL operands carry a query and a weight (1: bf16 calls, 3: fp32).
+template <int D, int QT, int PL>
+struct KvqRows {
+  static constexpr bool HALF = PL == 1;  // weights in fp16
+  bf16x8 q[QT][PL][D / 32];
+  floatx4 O[QT][D / 16];
+  float m[QT], R[QT], l[QT];
+  int pos[QT];  // last position that this lane's row sees (-1: none)
+
+  __device__ __forceinline__ void start() {
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+      m[i] = R[i] = KVQ_NONE;
+      l[i] = 0.f;
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt) O[i][dt] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
   }
-  part[tid] = acc;
+
+  // query operands of row r (-1: none) of tile i: lane group c, operand 2 u + w, element e is dim 64 u + 16 c + 8 w + e
+  template <typename E>
+  __device__ __forceinline__ void load_q(int i, const E* row, bool neg) {
+    const int c = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int kd = 0; kd < D / 32; ++kd) {
+      const E* p = row + 64 * (kd >> 1) + 16 * c + 8 * (kd & 1);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float x = row ? kvq_ld(p + e) : 0.f;
+        if (neg) x = -x;
+#pragma unroll
+        for (int pl = 0; pl < PL; ++pl) {  // (the last rounding of three takes what is left: 24 bits)
+          const uint16_t b = f2bf(x);
+          q[i][pl][kd][e] = __builtin_bit_cast(__bf16, b);
+          x -= bf2f(b);
+        }
+      }
+    }
+  }
+
+  // what takes the sums from R (and the codes' exponents) to m
+  __device__ __forceinline__ float to_m(int i) const { return HALF ? exp2f(R[i] - m[i] - 127.f) : 1.f; }
+
+  // one step: keys j0 .. j0 + 63
+  template <bool MASK>
+  __device__ __forceinline__ void step(const KvqStage<D>& s, int j0, int kend, float sc) {
+    const int c = (threadIdx.x & 63) >> 4;
+    floatx4 S[QT][4];
+    const float ks = kvq_pow2(s.ek - 127);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+#pragma unroll
+      for (int i = 0; i < QT; ++i) S[i][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int u = 0; u < D / 64; ++u) {
+        const bf16x8 k0 = kvq_bf16x8(s.k[t][u].x, s.k[t][u].y, ks), k1 = kvq_bf16x8(s.k[t][u].z, s.k[t][u].w, ks);
+#pragma unroll
+        for (int i = 0; i < QT; ++i)
+#pragma unroll
+          for (int pl = PL - 1; pl >= 0; --pl) {  // small parts first
+            S[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q[i][pl][2 * u], S[i][t], 0, 0, 0);
+            S[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[i][pl][2 * u + 1], S[i][t], 0, 0, 0);
+          }
+      }
+    }
+    typedef std::conditional_t<HALF, kvq_h8, bf16x8> W8;
+    W8 P[QT][PL][2];
+    const float ev = (float)s.ev;
+#pragma unroll
+    for (int i = 0; i < QT; ++i) {
+      if constexpr (MASK) {
+        const int last = s.ev < 0 ? -1 : min(pos[i], kend - 1), key = j0 + 16 * c;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) S[i][t][e] = key + 4 * t + e <= last ? S[i][t][e] : -INFINITY;
+      }
+      float x = fmaxf(fmaxf(S[i][0][0], S[i][0][1]), fmaxf(S[i][0][2], S[i][0][3]));
+#pragma unroll
+      for (int t = 1; t < 4; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x = fmaxf(x, S[i][t][e]);
+      x *= sc;
+      const float mx = kvq_max_groups(x), rx = HALF ? kvq_max_groups(x + ev) - KVQ_LIFT : mx;
+      if (__any(mx > m[i] + KVQ_LAZY || rx > R[i] + KVQ_LAZY)) {
+        const float mn = fmaxf(m[i], mx), rn = fmaxf(R[i], rx), fr = exp2f(R[i] - rn);
+        l[i] *= exp2f(m[i] - mn);
+#pragma unroll
+        for (int dt = 0; dt < D / 16; ++dt) O[i][dt] *= fr;
+        m[i] = mn;
+        R[i] = rn;
+      }
+      // (the clamp: a factor that large only meets weights below fp32's range)
+      const float f = HALF ? __builtin_amdgcn_exp2f(fminf(ev + m[i] - R[i], 100.f)) : 1.f;
+      float ls = 0.f;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(fmaf(S[i][t][e], sc, -m[i]));
+          ls += p[e];
+          if constexpr (HALF) p[e] *= f;
+        }
+#pragma unroll
+        for (int pl = 0; pl < PL; ++pl)
+#pragma unroll
+          for (int e = 0; e < 4; e += 2) {
+            const auto w = __builtin_convertvector(kvq_f2{p[e], p[e + 1]}, std::conditional_t<HALF, kvq_h2, bf16x2>);
+            P[i][pl][t >> 1][4 * (t & 1) + e] = w[0];
+            P[i][pl][t >> 1][4 * (t & 1) + e + 1] = w[1];
+            p[e] -= (float)w[0];
+            p[e + 1] -= (float)w[1];
+          }
+      }
+      l[i] += ls;
+    }
+    // codes that no row sees may be anything: zero in their place
+    uint32_t keep[4];
+    if constexpr (MASK) {
+      const int n = s.ev < 0 ? 0 : kend - (j0 + 16 * c);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const int nb = n - 4 * w;
+        keep[w] = nb >= 4 ? ~0u : nb <= 0 ? 0u : (1u << (8 * nb)) - 1u;
+      }
+    }
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) {
+      uint4 v = s.v[dt];
+      if constexpr (MASK) v.x &= keep[0], v.y &= keep[1], v.z &= keep[2], v.w &= keep[3];
+      if constexpr (HALF) {
+        const kvq_h8 v0 = kvq_f16x8(v.x, v.y), v1 = kvq_f16x8(v.z, v.w);
+#pragma unroll
+        for (int i = 0; i < QT; ++i) {
+          O[i][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, P[i][0][0], O[i][dt], 0, 0, 0);
+          O[i][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, P[i][0][1], O[i][dt], 0, 0, 0);
+        }
+      } else {
+        const float vs = kvq_pow2(max(s.ev, 1) - 127);
+        const bf16x8 v0 = kvq_bf16x8(v.x, v.y, vs), v1 = kvq_bf16x8(v.z, v.w, vs);
+#pragma unroll
+        for (int i = 0; i < QT; ++i)
+#pragma unroll
+          for (int pl = PL - 1; pl >= 0; --pl) {
+            O[i][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, P[i][pl][0], O[i][dt], 0, 0, 0);
+            O[i][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, P[i][pl][1], O[i][dt], 0, 0, 0);
+          }
+      }
+    }
+  }
+};
+
+// Rows and keys of one request under a launch: the same arithmetic in the attention and the merge kernel.
+struct KvqGeom {
+  int r0, n;       // first row of q, rows (at most max_q)
+  int n_rows;
+  int first;       // position of row 0
+  int chunk;       // keys of a split
+  int limit;       // positions that exist for the table
+  __device__ __forceinline__ KvqGeom(const KvqAttnArgs& a, int b) {
+    const int c0 = a.cu[b], len = a.lens[b];
+    const long long all = (long long)a.cu[b + 1] - c0, f = (long long)len - all;
+    r0 = c0;
+    n_rows = a.n_rows;
+    n = (int)max(0ll, min(all, (long long)a.max_q));
+    first = (int)max(f, (long long)INT_MIN / 2);
+    limit = (int)max(0ll, min((long long)a.width * a.T, (long long)len));
+    chunk = ((limit + a.nsplit - 1) / a.nsplit + KVQ_STEP - 1) & ~(KVQ_STEP - 1);
+    if (chunk < KVQ_STEP) chunk = KVQ_STEP;
+  }
+  // row i is one of q's
+  __device__ __forceinline__ bool has(int i) const { return (unsigned long long)((long long)r0 + i) < (unsigned long long)n_rows; }
+  // keys seen by the last row of rows [r, r + rows) of the request's n * g
+  __device__ __forceinline__ int keys(int r, int rows, int g) const {
+    const int last = min(r + rows, n * g) - 1;
+    return max(0, min(limit, first + last / g + 1));
+  }
+};
+
+// Waves split the keys: a workgroup of four owns 16 QT rows of one (request, KV head)
+// and one share of its keys; wave w takes every fourth step, a step's codes in
+// registers while the next step's are on their way, and the four meet in LDS.
+// For few rows, where the cache's bytes bound it.
+template <typename E, int D, int QT>
+__global__ __launch_bounds__(256) void kvq_attn_keys_kernel(KvqAttnArgs a) {
+  constexpr int ROWS = 16 * QT, RS = D + 4;
+  __shared__ __align__(16) float so[4 * ROWS * RS];
+  __shared__ float sm[4 * ROWS], sl[4 * ROWS];
+  const int g = a.Hq / a.Hkv;
+  int w = blockIdx.x;
+  const int h = w % a.Hkv;
+  w /= a.Hkv;
+  const int grp = w % a.groups;
+  w /= a.groups;
+  const int split = w % a.nsplit, b = w / a.nsplit;
+  const KvqGeom ge(a, b);
+  const int R = ge.n * g, rb = grp * ROWS;
+  if (rb >= R) return;
+  const int kall = ge.keys(rb, ROWS, g), active = max(1, (kall + ge.chunk - 1) / ge.chunk);
+  if (split >= active) return;
+  const int kbeg = split * ge.chunk, kend = min(kbeg + ge.chunk, kall);
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, c = lane >> 4;
+  const float sc = a.scale_log2;
+  KvqRows<D, QT, sizeof(E) == 2 ? 1 : 3> rows;
+  rows.start();
+#pragma unroll
+  for (int i = 0; i < QT; ++i) {
+    const int r = rb + 16 * i + col;
+    const E* src = nullptr;
+    rows.pos[i] = -1;
+    if (r < R && ge.has(r / g)) {
+      rows.pos[i] = ge.first + r / g;
+      src = (const E*)a.q + (size_t)(ge.r0 + r / g) * a.ld_q + (size_t)(h * g + r % g) * D;
+    }
+    rows.load_q(i, src, a.neg);
+  }
+  const int seen_all = min(kend, ge.first + rb / g + 1);  // keys below this are seen by every row
+  const KvqWalk<D> walk(a, b, h, kend);
+  const int first = kbeg + wave * KVQ_STEP, nit = first < kend ? (kend - first + 4 * KVQ_STEP - 1) / (4 * KVQ_STEP) : 0;
+  auto key = [&](int it) { return first + it * 4 * KVQ_STEP; };
+  auto work = [&](const KvqStage<D>& s, int j0) {
+    if (j0 + KVQ_STEP <= seen_all && __all(s.ev >= 0)) rows.template step<false>(s, j0, kend, sc);
+    else rows.template step<true>(s, j0, kend, sc);
+  };
+  if (nit > 0) {
+    KvqStage<D> sa, sb;
+    KvqPlace p0 = walk.place(key(0)), p1 = walk.place(key(1));
+    walk.load(sa, key(0), p0);
+    for (int it = 0; it < nit; it += 2) {
+      p0 = walk.place(key(it + 2));
+      walk.load(sb, key(it + 1), p1);
+      work(sa, key(it));
+      p1 = walk.place(key(it + 3));
+      walk.load(sa, key(it + 2), p0);
+      if (it + 1 < nit) work(sb, key(it + 1));
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < QT; ++i) {
+    float l = rows.l[i];
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    const float f = rows.to_m(i);
+    float* row = so + (size_t)(wave * ROWS + 16 * i + col) * RS;
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) *(floatx4*)(row + 16 * dt + 4 * c) = rows.O[i][dt] * f;
+    if (c == 0) {
+      sm[wave * ROWS + 16 * i + col] = rows.m[i];
+      sl[wave * ROWS + 16 * i + col] = l;
+    }
+  }
   __syncthreads();
-  if (tid < D) {
-    for (int t = 1; t < np; ++t) acc += part[t * D + tid];
-    const float o = l > 0.f ? acc / l : 0.f;
-    E* dst = (E*)a.o + row * a.ld_o + (size_t)hq * D + tid;
-    if constexpr (sizeof(E) == 2) *dst = f2bf(o);
-    else *dst = o;
+  const size_t part = (((size_t)b * a.Hkv + h) * a.nsplit + split) * a.rows_pad + rb;
+  for (int i = tid; i < ROWS * (D / 4); i += 256) {
+    const int r = i / (D / 4), d = 4 * (i % (D / 4));
+    if (rb + r >= R || !ge.has((rb + r) / g)) continue;
+    float M = sm[r];
+#pragma unroll
+    for (int v = 1; v < 4; ++v) M = fmaxf(M, sm[v * ROWS + r]);
+    float L = 0.f;
+    floatx4 o = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      const float e = exp2f(sm[v * ROWS + r] - M);
+      L += sl[v * ROWS + r] * e;
+      o += *(const floatx4*)(so + (size_t)(v * ROWS + r) * RS + d) * e;
+    }
+    if (active == 1) {
+      kvq_store4((E*)a.o + (size_t)(ge.r0 + (rb + r) / g) * a.ld_o + (size_t)(h * g + (rb + r) % g) * D + d, o, L);
+    } else {
+      *(floatx4*)(a.part_o + (part + r) * D + d) = o;
+      if (d == 0) a.part_s[part + r] = make_float2(M, L);
+    }
   }
 }
 
-size_t kvq_attn_workspace(const KvqAttnArgs&) { return 0; }
+// Joins the splits of rows that have more than one: a wave a row and query head.
+template <typename E, int D>
+__global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttnArgs a) {
+  const int g = a.Hq / a.Hkv, lane = threadIdx.x & 63;
+  const long long w = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int r = (int)(w % (a.max_q * g)), h = (int)(w / (a.max_q * g) % a.Hkv), b = (int)(w / (a.max_q * g) / a.Hkv);
+  if (b >= a.B) return;
+  const KvqGeom ge(a, b);
+  if (r >= ge.n * g || !ge.has(r / g)) return;
+  const int kall = ge.keys(r / a.group_rows * a.group_rows, a.group_rows, g), active = (kall + ge.chunk - 1) / ge.chunk;
+  if (active <= 1) return;
+  const size_t part = ((size_t)b * a.Hkv + h) * a.nsplit * a.rows_pad + r;
+  float M = -INFINITY;
+  for (int s = lane; s < active; s += 64) M = fmaxf(M, a.part_s[part + (size_t)s * a.rows_pad].x);
+  for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
+  constexpr int N = D / 64;
+  float acc[N] = {}, L = 0.f;
+  for (int s = 0; s < active; ++s) {
+    const float2 st = a.part_s[part + (size_t)s * a.rows_pad];
+    const float e = exp2f(st.x - M);
+    L += st.y * e;
+    const float* p = a.part_o + (part + (size_t)s * a.rows_pad) * D + lane * N;
+#pragma unroll
+    for (int j = 0; j < N; ++j) acc[j] = fmaf(p[j], e, acc[j]);
+  }
+  const float inv = L > 0.f ? 1.f / L : 0.f;
+  E* dst = (E*)a.o + (size_t)(ge.r0 + r / g) * a.ld_o + (size_t)(h * g + r % g) * D + lane * N;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    if constexpr (sizeof(E) == 2) dst[j] = f2bf(acc[j] * inv);
+    else dst[j] = acc[j] * inv;
+  }
+}
 
-void kvq_attention(const KvqAttnArgs& a, hipStream_t st) {
-  const dim3 grid((unsigned)((long long)a.B * a.max_q), a.Hq);
-  if (a.bf16) hipLaunchKernelGGL(kvq_attn_kernel<uint16_t>, grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(kvq_attn_kernel<float>, grid, dim3(256), 0, st, a);
+// How a call is split (host): 16-row tiles a wave, row groups, and shares of the keys.
+void kvq_attn_plan(KvqAttnArgs& a) {
+  const int rows = a.max_q * (a.Hq / a.Hkv);
+  a.qt = rows > 16 && a.bf16 ? 2 : 1;
+  a.group_rows = 16 * a.qt;
+  a.groups = (rows + a.group_rows - 1) / a.group_rows;
+  a.rows_pad = a.groups * a.group_rows;
+  // enough workgroups to fill the chip, each with at least two rounds of its waves' steps
+  const long long base = (long long)a.B * a.Hkv * a.groups;
+  const long long most = std::max<long long>(1, a.max_len / (8 * KVQ_STEP));
+  a.nsplit = (int)std::max<long long>(1, std::min<long long>({most, (4096 + base - 1) / base, 64}));
+}
+
+static size_t kvq_part_rows(const KvqAttnArgs& a) { return (size_t)a.B * a.Hkv * a.nsplit * a.rows_pad; }
+
+size_t kvq_attn_workspace(KvqAttnArgs a) {
+  kvq_attn_plan(a);
+  return a.nsplit > 1 ? kvq_part_rows(a) * (a.D + 2) * 4 : 0;
+}
+
+template <typename E, int D>
+static void kvq_launch(const KvqAttnArgs& a, hipStream_t st) {
+  const dim3 grid((unsigned)((long long)a.B * a.nsplit * a.groups * a.Hkv));
+  if constexpr (sizeof(E) == 2) {
+    if (a.qt == 2) hipLaunchKernelGGL((kvq_attn_keys_kernel<E, D, 2>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((kvq_attn_keys_kernel<E, D, 1>), grid, dim3(256), 0, st, a);
+  } else {
+    hipLaunchKernelGGL((kvq_attn_keys_kernel<E, D, 1>), grid, dim3(256), 0, st, a);
+  }
+  if (a.nsplit > 1) {
+    const long long rows = (long long)a.B * a.Hkv * a.max_q * (a.Hq / a.Hkv);
+    hipLaunchKernelGGL((kvq_merge_kernel<E, D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a);
+  }
+}
+
+void kvq_attention(KvqAttnArgs a, hipStream_t st) {
+  kvq_attn_plan(a);
+  a.part_o = (float*)a.workspace;
+  a.part_s = (float2*)(a.part_o + kvq_part_rows(a) * a.D);
+  // a negative scale turns the queries' signs; scores of a zero one are all 0 (not 0 * -inf where a key is hidden)
+  a.neg = a.scale < 0.f;
+  a.scale_log2 = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-37f);
+  if (a.bf16) {
+    if (a.D == 128) kvq_launch<uint16_t, 128>(a, st);
+    else kvq_launch<uint16_t, 64>(a, st);
+  } else {
+    if (a.D == 128) kvq_launch<float, 128>(a, st);
+    else kvq_launch<float, 64>(a, st);
+  }
 }
 
 }  // namespace ssd

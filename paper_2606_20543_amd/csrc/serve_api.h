@@ -71,8 +71,10 @@ ssd_status attn_sizes(const ssd_kvq_cache* c, const ssd_kvq_attn_params* p, KvqA
     return fail(SSD_E_INVAL, "n_seqs, n_rows, max_q, max_len and table_width must be positive");
   if (p->n_heads < 1 || p->n_heads % c->n_kv_heads || p->n_heads > 65535)
     return fail(SSD_E_INVAL, "n_heads = %d must be a multiple of n_kv_heads = %d", p->n_heads, c->n_kv_heads);
-  if ((int64_t)p->n_seqs * p->max_q > INT32_MAX)
-    return fail(SSD_E_INVAL, "n_seqs * max_q must stay below 2^31");
+  if ((int64_t)p->n_seqs * p->max_q > INT32_MAX / p->n_heads)
+    return fail(SSD_E_INVAL, "n_seqs * max_q * n_heads must stay below 2^31");
+  if ((int64_t)p->table_width * c->block > (1 << 30))
+    return fail(SSD_E_INVAL, "table_width * block must be at most 2^30 positions");
   const int64_t cols = (int64_t)p->n_heads * c->head_dim;
   if (p->ld_q < cols || p->ld_out < cols) return fail(SSD_E_INVAL, "row lengths must be at least n_heads * head_dim");
   if (!std::isfinite(p->scale) || !std::isfinite((float)p->scale)) return fail(SSD_E_INVAL, "scale must be finite");

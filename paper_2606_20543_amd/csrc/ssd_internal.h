@@ -483,9 +483,14 @@ struct KvqAttnArgs {
   const int *cu, *lens, *table;
   float scale;
   void* workspace;
+  // the plan (kvq.h): row groups, key shares, partial results in the workspace
+  int qt, groups, group_rows, rows_pad, nsplit, neg;
+  float scale_log2;
+  float* part_o;   // [B][Hkv][nsplit][rows_pad][D], relative to the row's maximum
+  float2* part_s;  // [B][Hkv][nsplit][rows_pad] (maximum, log2 domain; sum)
 };
-size_t kvq_attn_workspace(const KvqAttnArgs& a);  // bytes
-void kvq_attention(const KvqAttnArgs& a, hipStream_t st);
+size_t kvq_attn_workspace(KvqAttnArgs a);  // bytes
+void kvq_attention(KvqAttnArgs a, hipStream_t st);
 
 // fill helpers (graph-capture safe)
 void fill_u32(unsigned* p, size_t n, unsigned v, hipStream_t st);

@@ -122,9 +122,9 @@ class Cache:
             a = e
 
     def gather(self, table_row, n, h):
-        """Keys, values [n][D] of KV head h and whether each position exists."""
+        """Keys, values [n][D] of KV head h, whether each position exists, and the largest value its block can hold."""
         D = self.k.shape[3]
-        K, V, ok = np.zeros((n, D)), np.zeros((n, D)), np.zeros(n, bool)
+        K, V, ok, top = np.zeros((n, D)), np.zeros((n, D)), np.zeros(n, bool), np.zeros(n)
         for p in range(n):
             j = p // self.block
             pg = table_row[j] if j < len(table_row) else -1
@@ -132,7 +132,8 @@ class Cache:
                 ok[p] = True
                 K[p] = self.k[pg, h, p % self.block] * 2.0 ** (self.ke[pg, h] - 127)
                 V[p] = self.v[pg, h, p % self.block] * 2.0 ** (self.ve[pg, h] - 127)
-        return K, V, ok
+                top[p] = 448.0 * 2.0 ** (self.ve[pg, h] - 127)
+        return K, V, ok, top
 
 
 def attention(cache, q, cu, lens, table, scale, bf16):
@@ -142,7 +143,9 @@ def attention(cache, q, cu, lens, table, scale, bf16):
     plus 4 2^-24 of itself (scaling, the subtraction of the maximum, the exponential's argument); an
     exponential by a few units more; its weight then by a factor of about 1 + d, the normalised one by twice that;
     the weighted sum of n values adds (n + 16) 2^-24 sum p |v|.  bf16 outputs add their own rounding,
-    2^-8 |o|, and may carry the weights in a type of 11 bits, 2^-11 sum p |v|.  A weight below 2^-126 of the
+    2^-8 |o|, and may carry the weights in a type of 11 bits, 2^-11 sum p |v|: fp16, whose smallest step is
+    2^-24, with the largest weight (times its block's value scale) held at 2^6 or above, so that a smaller one is
+    off by at most 2^-25 2^-6 of that, and a value by that times its code: n 2^-31 max (p scale) 448.  A weight below 2^-126 of the
     largest, and a result below 2^-126, has no normal fp32 value and may be 0: n 2^-126 max |v| + 2^-126.
     """
     rows, Hq, D = q.shape
@@ -155,7 +158,7 @@ def attention(cache, q, cu, lens, table, scale, bf16):
             continue
         L = max(0, min(int(lens[b]), table.shape[1] * cache.block))
         for h in range(cache.k.shape[1]):
-            K, V, ok = cache.gather(table[b], L, h)
+            K, V, ok, top = cache.gather(table[b], L, h)
             for i in range(n):
                 if not 0 <= r0 + i < rows:
                     continue
@@ -173,7 +176,8 @@ def attention(cache, q, cu, lens, table, scale, bf16):
                     pv = p @ np.abs(V[seen])
                     o = p @ V[seen]
                     out[r0 + i, j] = o
-                    tol[r0 + i, j] = pv * (2 * d + (L + 16) * u) + 2.0 ** -126 * (1 + L * np.abs(V[seen]).max()) + (np.abs(o) * 2.0 ** -8 + pv * 2.0 ** -11 if bf16 else 0.0)
+                    tol[r0 + i, j] = pv * (2 * d + (L + 16) * u) + 2.0 ** -126 * (1 + L * np.abs(V[seen]).max()) + (
+                        np.abs(o) * 2.0 ** -8 + pv * 2.0 ** -11 + L * 2.0 ** -31 * (p * top[seen]).max() if bf16 else 0.0)
     return out, tol
 
 

@@ -114,7 +114,7 @@ def test_attention_refusals(lib):
     cases += [(c, change(p, **kw), word) for kw, word in (
         (dict(dtype=-1), "dtype"), (dict(n_seqs=0), "positive"), (dict(n_rows=0), "positive"), (dict(max_q=0), "positive"),
         (dict(max_len=0), "positive"), (dict(table_width=0), "positive"), (dict(n_heads=5), "n_heads"), (dict(n_heads=0), "n_heads"),
-        (dict(n_seqs=2 ** 20, max_q=2 ** 20), "2^31"), (dict(ld_q=255), "row lengths"), (dict(ld_out=255), "row lengths"),
+        (dict(n_seqs=2 ** 15, max_q=2 ** 14), "2^31"), (dict(table_width=2 ** 27), "2^30"), (dict(ld_q=255), "row lengths"), (dict(ld_out=255), "row lengths"),
         (dict(scale=float("nan")), "scale"), (dict(scale=1e300), "scale"))]
     for cc, pp, word in cases:
         refused(ssd.ssd_kvq_attention, [cc, pp] + a, word)
