@@ -167,11 +167,68 @@ constexpr float KVQ_NONE = -1e30f;  // m and R before the first key
 constexpr float KVQ_LAZY = 8.f;
 constexpr float KVQ_LIFT = 6.f;     // p' of the largest lies at 2^6 (2^14 before R moves on): fp16 steps of 2^-30 of it
 
+__device__ __forceinline__ bf16x8 kvq_bf16x8(uint32_t lo, uint32_t hi, float scale) {
+  bf16x8 r;
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false),
+               b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true),
+               c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false),
+               d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+  r[0] = a[0], r[1] = a[1], r[2] = b[0], r[3] = b[1], r[4] = c[0], r[5] = c[1], r[6] = d[0], r[7] = d[1];
+  return r;
+}
+__device__ __forceinline__ kvq_h8 kvq_f16x8(uint32_t lo, uint32_t hi) {
+  kvq_h8 r;
+  const kvq_h2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true),
+               c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true);
+  r[0] = a[0], r[1] = a[1], r[2] = b[0], r[3] = b[1], r[4] = c[0], r[5] = c[1], r[6] = d[0], r[7] = d[1];
+  return r;
+}
+
 template <int D>
 struct KvqStage {
   uint4 k[4][D / 64];  // 16 codes of key (tile t, row lane % 16), dims 64 u + 16 (lane / 16) ..
   uint4 v[D / 16];     // 16 keys of dim 16 dt + lane % 16
   int ek, ev;          // exponents: of this lane's key rows, of its 16 keys (-1: not in the cache)
+};
+
+// Codes of positions that no row sees (key kend and on, blocks that are not there) may be
+// anything: what is left of 16 codes from key `key` on, zero in their place.
+struct KvqKeep {
+  uint32_t m[4];
+  __device__ __forceinline__ KvqKeep(int iev, int key, int kend) {
+    const int n = iev < 0 ? 0 : kend - key;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const int nb = n - 4 * w;
+      m[w] = nb >= 4 ? ~0u : nb <= 0 ? 0u : (1u << (8 * nb)) - 1u;
+    }
+  }
+  __device__ __forceinline__ uint4 operator()(uint4 v) const { return make_uint4(v.x & m[0], v.y & m[1], v.z & m[2], v.w & m[3]); }
+};
+
+// the operands of a step straight from a stage's codes; HALF: values as fp16 codes, else bf16 with their scale
+template <int D, bool HALF>
+struct KvqFromCodes {
+  const KvqStage<D>& s;
+  int key, kend;
+  __device__ __forceinline__ void keys(int t, int u, bf16x8& k0, bf16x8& k1) const {
+    const float ks = kvq_pow2(s.ek - 127);
+    k0 = kvq_bf16x8(s.k[t][u].x, s.k[t][u].y, ks);
+    k1 = kvq_bf16x8(s.k[t][u].z, s.k[t][u].w, ks);
+  }
+  template <bool MASK, typename W8>
+  __device__ __forceinline__ void values(int dt, W8& v0, W8& v1) const {
+    uint4 v = s.v[dt];
+    if constexpr (MASK) v = KvqKeep(s.ev, key, kend)(v);
+    if constexpr (HALF) {
+      v0 = kvq_f16x8(v.x, v.y);
+      v1 = kvq_f16x8(v.z, v.w);
+    } else {
+      const float vs = kvq_pow2(max(s.ev, 1) - 127);
+      v0 = kvq_bf16x8(v.x, v.y, vs);
+      v1 = kvq_bf16x8(v.z, v.w, vs);
+    }
+  }
 };
 
 // where a lane's 16 keys of a step lie
@@ -213,23 +270,6 @@ struct KvqWalk {
     if (pl.v < 0) s.ev = -1;
   }
 };
-
-__device__ __forceinline__ bf16x8 kvq_bf16x8(uint32_t lo, uint32_t hi, float scale) {
-  bf16x8 r;
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false),
-               b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true),
-               c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false),
-               d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
-  r[0] = a[0], r[1] = a[1], r[2] = b[0], r[3] = b[1], r[4] = c[0], r[5] = c[1], r[6] = d[0], r[7] = d[1];
-  return r;
-}
-__device__ __forceinline__ kvq_h8 kvq_f16x8(uint32_t lo, uint32_t hi) {
-  kvq_h8 r;
-  const kvq_h2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true),
-               c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true);
-  r[0] = a[0], r[1] = a[1], r[2] = b[0], r[3] = b[1], r[4] = c[0], r[5] = c[1], r[6] = d[0], r[7] = d[1];
-  return r;
-}
 
 // largest over the four lane groups, in every lane
 __device__ __forceinline__ float kvq_max_groups(float x) {
@@ -280,19 +320,19 @@ struct KvqRows {
   // what takes the sums from R (and the codes' exponents) to m
   __device__ __forceinline__ float to_m(int i) const { return HALF ? exp2f(R[i] - m[i] - 127.f) : 1.f; }
 
-  // one step: keys j0 .. j0 + 63
-  template <bool MASK>
-  __device__ __forceinline__ void step(const KvqStage<D>& s, int j0, int kend, float sc) {
+  // one step: keys j0 .. j0 + 63, their operands from src, iev the value exponent of this lane's keys
+  template <bool MASK, typename Src>
+  __device__ __forceinline__ void step(const Src& src, int iev, int j0, int kend, float sc) {
     const int c = (threadIdx.x & 63) >> 4;
     floatx4 S[QT][4];
-    const float ks = kvq_pow2(s.ek - 127);
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
 #pragma unroll
       for (int i = 0; i < QT; ++i) S[i][t] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int u = 0; u < D / 64; ++u) {
-        const bf16x8 k0 = kvq_bf16x8(s.k[t][u].x, s.k[t][u].y, ks), k1 = kvq_bf16x8(s.k[t][u].z, s.k[t][u].w, ks);
+        bf16x8 k0, k1;
+        src.keys(t, u, k0, k1);
 #pragma unroll
         for (int i = 0; i < QT; ++i)
 #pragma unroll
@@ -304,11 +344,11 @@ struct KvqRows {
     }
     typedef std::conditional_t<HALF, kvq_h8, bf16x8> W8;
     W8 P[QT][PL][2];
-    const float ev = (float)s.ev;
+    const float ev = (float)iev;
 #pragma unroll
     for (int i = 0; i < QT; ++i) {
       if constexpr (MASK) {
-        const int last = s.ev < 0 ? -1 : min(pos[i], kend - 1), key = j0 + 16 * c;
+        const int last = iev < 0 ? -1 : min(pos[i], kend - 1), key = j0 + 16 * c;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -354,38 +394,22 @@ struct KvqRows {
       }
       l[i] += ls;
     }
-    // codes that no row sees may be anything: zero in their place
-    uint32_t keep[4];
-    if constexpr (MASK) {
-      const int n = s.ev < 0 ? 0 : kend - (j0 + 16 * c);
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const int nb = n - 4 * w;
-        keep[w] = nb >= 4 ? ~0u : nb <= 0 ? 0u : (1u << (8 * nb)) - 1u;
-      }
-    }
 #pragma unroll
     for (int dt = 0; dt < D / 16; ++dt) {
-      uint4 v = s.v[dt];
-      if constexpr (MASK) v.x &= keep[0], v.y &= keep[1], v.z &= keep[2], v.w &= keep[3];
-      if constexpr (HALF) {
-        const kvq_h8 v0 = kvq_f16x8(v.x, v.y), v1 = kvq_f16x8(v.z, v.w);
+      W8 v0, v1;
+      src.template values<MASK>(dt, v0, v1);
 #pragma unroll
-        for (int i = 0; i < QT; ++i) {
-          O[i][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, P[i][0][0], O[i][dt], 0, 0, 0);
-          O[i][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, P[i][0][1], O[i][dt], 0, 0, 0);
-        }
-      } else {
-        const float vs = kvq_pow2(max(s.ev, 1) - 127);
-        const bf16x8 v0 = kvq_bf16x8(v.x, v.y, vs), v1 = kvq_bf16x8(v.z, v.w, vs);
+      for (int i = 0; i < QT; ++i)
 #pragma unroll
-        for (int i = 0; i < QT; ++i)
-#pragma unroll
-          for (int pl = PL - 1; pl >= 0; --pl) {
+        for (int pl = PL - 1; pl >= 0; --pl) {
+          if constexpr (HALF) {
+            O[i][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, P[i][pl][0], O[i][dt], 0, 0, 0);
+            O[i][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, P[i][pl][1], O[i][dt], 0, 0, 0);
+          } else {
             O[i][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, P[i][pl][0], O[i][dt], 0, 0, 0);
             O[i][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, P[i][pl][1], O[i][dt], 0, 0, 0);
           }
-      }
+        }
     }
   }
 };
@@ -405,8 +429,7 @@ struct KvqGeom {
     n = (int)max(0ll, min(all, (long long)a.max_q));
     first = (int)max(f, (long long)INT_MIN / 2);
     limit = (int)max(0ll, min((long long)a.width * a.T, (long long)len));
-    chunk = ((limit + a.nsplit - 1) / a.nsplit + KVQ_STEP - 1) & ~(KVQ_STEP - 1);
-    if (chunk < KVQ_STEP) chunk = KVQ_STEP;
+    chunk = max(a.chunk, ((limit + a.nsplit - 1) / a.nsplit + KVQ_STEP - 1) & ~(KVQ_STEP - 1));
   }
   // row i is one of q's
   __device__ __forceinline__ bool has(int i) const { return (unsigned long long)((long long)r0 + i) < (unsigned long long)n_rows; }
@@ -459,8 +482,9 @@ __global__ __launch_bounds__(256) void kvq_attn_keys_kernel(KvqAttnArgs a) {
   const int first = kbeg + wave * KVQ_STEP, nit = first < kend ? (kend - first + 4 * KVQ_STEP - 1) / (4 * KVQ_STEP) : 0;
   auto key = [&](int it) { return first + it * 4 * KVQ_STEP; };
   auto work = [&](const KvqStage<D>& s, int j0) {
-    if (j0 + KVQ_STEP <= seen_all && __all(s.ev >= 0)) rows.template step<false>(s, j0, kend, sc);
-    else rows.template step<true>(s, j0, kend, sc);
+    const KvqFromCodes<D, sizeof(E) == 2> src{s, j0 + 16 * c, kend};
+    if (j0 + KVQ_STEP <= seen_all && __all(s.ev >= 0)) rows.template step<false>(src, s.ev, j0, kend, sc);
+    else rows.template step<true>(src, s.ev, j0, kend, sc);
   };
   if (nit > 0) {
     KvqStage<D> sa, sb;
@@ -514,6 +538,142 @@ __global__ __launch_bounds__(256) void kvq_attn_keys_kernel(KvqAttnArgs a) {
   }
 }
 
+// Waves split the rows: a workgroup of four owns 128 rows of one (request, KV head) and
+// one share of its keys.  A step's codes are converted once for all waves, a
+// quarter each, into operands in LDS (32 KB at D = 128, two steps' worth), while
+// the codes of the step after next are on their way in registers; every wave
+// multiplies the whole step with its own two tiles of 16 rows.  bf16 calls with
+// many rows, where the matrix cores and the exponentials bound it.
+template <int D>
+struct KvqFromLds {
+  const uint16_t* st;  // operands of 64 x 16 bytes: keys (t, kd), then values (dt, half)
+  int lane;
+  __device__ __forceinline__ void keys(int t, int u, bf16x8& k0, bf16x8& k1) const {
+    const uint16_t* p = st + ((t * (D / 32) + 2 * u) * 64 + lane) * 8;
+    k0 = *(const bf16x8*)p;
+    k1 = *(const bf16x8*)(p + 512);
+  }
+  template <bool MASK>
+  __device__ __forceinline__ void values(int dt, kvq_h8& v0, kvq_h8& v1) const {
+    const uint16_t* p = st + ((4 * (D / 32) + 2 * dt) * 64 + lane) * 8;
+    v0 = *(const kvq_h8*)p;
+    v1 = *(const kvq_h8*)(p + 512);
+  }
+};
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void kvq_attn_rows_kernel(KvqAttnArgs a) {
+  constexpr int QT = 2, WROWS = 16 * QT, ROWS = 4 * WROWS, OPS = 4 * (D / 32) + 2 * (D / 16), DTW = D / 64;
+  __shared__ __align__(16) uint16_t sm[2 * OPS * 512];
+  const int g = a.Hq / a.Hkv;
+  int w = blockIdx.x;
+  const int h = w % a.Hkv;
+  w /= a.Hkv;
+  const int grp = w % a.groups;
+  w /= a.groups;
+  const int split = w % a.nsplit, b = w / a.nsplit;
+  const KvqGeom ge(a, b);
+  const int R = ge.n * g, rb = grp * ROWS;
+  if (rb >= R) return;
+  const int kall = ge.keys(rb, ROWS, g), active = max(1, (kall + ge.chunk - 1) / ge.chunk);
+  if (split >= active) return;
+  const int kbeg = split * ge.chunk, kend = min(kbeg + ge.chunk, kall);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, c = lane >> 4;
+  const float sc = a.scale_log2;
+  KvqRows<D, QT, 1> rows;
+  rows.start();
+  const int wr = rb + wave * WROWS;
+#pragma unroll
+  for (int i = 0; i < QT; ++i) {
+    const int r = wr + 16 * i + col;
+    const uint16_t* src = nullptr;
+    rows.pos[i] = -1;
+    if (r < R && ge.has(r / g)) {
+      rows.pos[i] = ge.first + r / g;
+      src = (const uint16_t*)a.q + (size_t)(ge.r0 + r / g) * a.ld_q + (size_t)(h * g + r % g) * D;
+    }
+    rows.load_q(i, src, a.neg);
+  }
+  const int seen_all = min(kend, ge.first + min(wr, R - 1) / g + 1);  // keys below this are seen by every row of the wave
+  const KvqWalk<D> walk(a, b, h, kend);
+  const int nit = (kend - kbeg + KVQ_STEP - 1) / KVQ_STEP;
+  // this wave's quarter of a step: key tile `wave`, DTW dim tiles of the values
+  uint4 ck[D / 64], cv[DTW];
+  int ek = 127, ev = -1;
+  auto load = [&](int j0, const KvqPlace& pl) {
+    const int T = a.T, pk = max(pl.k, 0), pv = max(pl.v, 0);
+    const uint8_t* kb = a.kc + (size_t)pk * walk.blk +
+                        (size_t)(h * T + ((j0 + 16 * (col >> 2)) & (T - 1)) + 4 * wave + (col & 3)) * D + 16 * c;
+    const uint8_t* vb = a.vc + (size_t)pv * walk.blk + (size_t)(h * D + 16 * DTW * wave + col) * T + ((j0 + 16 * c) & (T - 1));
+#pragma unroll
+    for (int u = 0; u < D / 64; ++u) ck[u] = *(const uint4*)(kb + 64 * u);
+#pragma unroll
+    for (int d = 0; d < DTW; ++d) cv[d] = *(const uint4*)(vb + (size_t)(16 * d) * T);
+    ek = a.ke[(size_t)pk * a.Hkv + h];
+    ev = a.ve[(size_t)pv * a.Hkv + h];
+    if (pl.k < 0) ek = 127;
+    if (pl.v < 0) ev = -1;
+  };
+  auto store = [&](int j0, uint16_t* st) {
+    const float ks = kvq_pow2(ek - 127);
+#pragma unroll
+    for (int u = 0; u < D / 64; ++u) {
+      uint16_t* p = st + ((wave * (D / 32) + 2 * u) * 64 + lane) * 8;
+      *(bf16x8*)p = kvq_bf16x8(ck[u].x, ck[u].y, ks);
+      *(bf16x8*)(p + 512) = kvq_bf16x8(ck[u].z, ck[u].w, ks);
+    }
+    const KvqKeep keep(ev, j0 + 16 * c, kend);
+#pragma unroll
+    for (int d = 0; d < DTW; ++d) {
+      uint16_t* p = st + ((4 * (D / 32) + 2 * (wave * DTW + d)) * 64 + lane) * 8;
+      const uint4 v = keep(cv[d]);
+      *(kvq_h8*)p = kvq_f16x8(v.x, v.y);
+      *(kvq_h8*)(p + 512) = kvq_f16x8(v.z, v.w);
+    }
+  };
+  if (nit > 0) {
+    KvqPlace pl = walk.place(kbeg + KVQ_STEP);
+    load(kbeg, walk.place(kbeg));
+    store(kbeg, sm);
+    int ev_now = ev;
+    load(kbeg + KVQ_STEP, pl);
+    pl = walk.place(kbeg + 2 * KVQ_STEP);
+    for (int it = 0; it < nit; ++it) {
+      const int j0 = kbeg + it * KVQ_STEP;
+      __syncthreads();  // step it is in its stage, and every wave is done with the other
+      const int ev_next = ev;
+      if (it + 1 < nit) {
+        store(j0 + KVQ_STEP, sm + ((it + 1) & 1) * OPS * 512);
+        load(j0 + 2 * KVQ_STEP, pl);
+        pl = walk.place(j0 + 3 * KVQ_STEP);
+      }
+      const KvqFromLds<D> src{sm + (it & 1) * OPS * 512, lane};
+      if (j0 + KVQ_STEP <= seen_all && __all(ev_now >= 0)) rows.template step<false>(src, ev_now, j0, kend, sc);
+      else rows.template step<true>(src, ev_now, j0, kend, sc);
+      ev_now = ev_next;
+    }
+  }
+  const size_t part = (((size_t)b * a.Hkv + h) * a.nsplit + split) * a.rows_pad;
+#pragma unroll
+  for (int i = 0; i < QT; ++i) {
+    float l = rows.l[i];
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    const float f = rows.to_m(i);
+    const int r = wr + 16 * i + col;
+    if (r >= R || !ge.has(r / g)) continue;
+    if (active == 1) {
+      uint16_t* dst = (uint16_t*)a.o + (size_t)(ge.r0 + r / g) * a.ld_o + (size_t)(h * g + r % g) * D + 4 * c;
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt) kvq_store4(dst + 16 * dt, rows.O[i][dt] * f, l);
+    } else {
+#pragma unroll
+      for (int dt = 0; dt < D / 16; ++dt) *(floatx4*)(a.part_o + (part + r) * D + 16 * dt + 4 * c) = rows.O[i][dt] * f;
+      if (c == 0) a.part_s[part + r] = make_float2(rows.m[i], l);
+    }
+  }
+}
+
 // Joins the splits of rows that have more than one: a wave a row and query head.
 template <typename E, int D>
 __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttnArgs a) {
@@ -548,17 +708,16 @@ __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttnArgs a) {
   }
 }
 
-// How a call is split (host): 16-row tiles a wave, row groups, and shares of the keys.
+// How a call is split (host): rows of a workgroup, and shares of the keys.
 void kvq_attn_plan(KvqAttnArgs& a) {
   const int rows = a.max_q * (a.Hq / a.Hkv);
+  a.by_rows = a.bf16 && rows > 64;
   a.qt = rows > 16 && a.bf16 ? 2 : 1;
-  a.group_rows = 16 * a.qt;
+  a.group_rows = a.by_rows ? 128 : 16 * a.qt;
   a.groups = (rows + a.group_rows - 1) / a.group_rows;
   a.rows_pad = a.groups * a.group_rows;
-  // enough workgroups to fill the chip, each with at least two rounds of its waves' steps
-  const long long base = (long long)a.B * a.Hkv * a.groups;
-  const long long most = std::max<long long>(1, a.max_len / (8 * KVQ_STEP));
-  a.nsplit = (int)std::max<long long>(1, std::min<long long>({most, (4096 + base - 1) / base, 64}));
+  a.chunk = a.by_rows ? 512 : 1024;
+  a.nsplit = std::max(1, std::min(64, (a.max_len + a.chunk - 1) / a.chunk));
 }
 
 static size_t kvq_part_rows(const KvqAttnArgs& a) { return (size_t)a.B * a.Hkv * a.nsplit * a.rows_pad; }
@@ -572,7 +731,8 @@ template <typename E, int D>
 static void kvq_launch(const KvqAttnArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)((long long)a.B * a.nsplit * a.groups * a.Hkv));
   if constexpr (sizeof(E) == 2) {
-    if (a.qt == 2) hipLaunchKernelGGL((kvq_attn_keys_kernel<E, D, 2>), grid, dim3(256), 0, st, a);
+    if (a.by_rows) hipLaunchKernelGGL((kvq_attn_rows_kernel<D>), grid, dim3(256), 0, st, a);
+    else if (a.qt == 2) hipLaunchKernelGGL((kvq_attn_keys_kernel<E, D, 2>), grid, dim3(256), 0, st, a);
     else hipLaunchKernelGGL((kvq_attn_keys_kernel<E, D, 1>), grid, dim3(256), 0, st, a);
   } else {
     hipLaunchKernelGGL((kvq_attn_keys_kernel<E, D, 1>), grid, dim3(256), 0, st, a);
