@@ -157,8 +157,9 @@ void kvq_append(const KvqAppendArgs& a, hipStream_t st) {
 // the weights take the value scale along, p' = 2^(t + e - R), e the value exponent of the
 // key's block and R a running bound of t + e, so that the codes themselves, exact in fp16,
 // are the other operand whatever the scales of different blocks are; p' is rounded to fp16,
-// 11 bits where the output has 8.  m and R follow their maxima lazily: the
-// sums are rescaled only where one has grown by more than 2^8.
+// 11 bits where the output has 8.  p' is formed alone, a lane's 16 of a step share e, so l takes
+// their sum times 2^(R - e - m).  m and R follow their maxima lazily: only where a lane
+// finds one grown by more than 2^8 are the maxima of all lanes taken and the sums rescaled.
 typedef _Float16 kvq_h8 __attribute__((ext_vector_type(8)));
 typedef _Float16 kvq_h2 __attribute__((ext_vector_type(2)));
 
@@ -188,7 +189,8 @@ template <int D>
 struct KvqStage {
   uint4 k[4][D / 64];  // 16 codes of key (tile t, row lane % 16), dims 64 u + 16 (lane / 16) ..
   uint4 v[D / 16];     // 16 keys of dim 16 dt + lane % 16
-  int ek, ev;          // exponents: of this lane's key rows, of its 16 keys (-1: not in the cache)
+  int ek, ev;          // exponents of this lane's key rows and of its 16 keys
+  bool has;            // its 16 keys begin inside the context, in a block of the cache
 };
 
 // Codes of positions that no row sees (key kend and on, blocks that are not there) may be
@@ -210,7 +212,7 @@ struct KvqKeep {
 template <int D, bool HALF>
 struct KvqFromCodes {
   const KvqStage<D>& s;
-  int key, kend;
+  int ev, key, kend;
   __device__ __forceinline__ void keys(int t, int u, bf16x8& k0, bf16x8& k1) const {
     const float ks = kvq_pow2(s.ek - 127);
     k0 = kvq_bf16x8(s.k[t][u].x, s.k[t][u].y, ks);
@@ -219,12 +221,12 @@ struct KvqFromCodes {
   template <bool MASK, typename W8>
   __device__ __forceinline__ void values(int dt, W8& v0, W8& v1) const {
     uint4 v = s.v[dt];
-    if constexpr (MASK) v = KvqKeep(s.ev, key, kend)(v);
+    if constexpr (MASK) v = KvqKeep(ev, key, kend)(v);
     if constexpr (HALF) {
       v0 = kvq_f16x8(v.x, v.y);
       v1 = kvq_f16x8(v.z, v.w);
     } else {
-      const float vs = kvq_pow2(max(s.ev, 1) - 127);
+      const float vs = kvq_pow2(max(ev, 1) - 127);
       v0 = kvq_bf16x8(v.x, v.y, vs);
       v1 = kvq_bf16x8(v.z, v.w, vs);
     }
@@ -233,7 +235,7 @@ struct KvqFromCodes {
 
 // where a lane's 16 keys of a step lie
 struct KvqPlace {
-  int k, v;  // blocks of the key rows' group and of the value group; -1: none
+  int k, v;  // table entries of the key rows' group and of the value group
 };
 
 template <int D>
@@ -245,32 +247,38 @@ struct KvqWalk {
   __device__ __forceinline__ KvqWalk(const KvqAttnArgs& args, int b, int head, int end)
       : a(args), trow(args.table + (size_t)b * args.width), h(head), lane(threadIdx.x & 63), kend(end),
         sh(__builtin_ctz(args.T)), blk((size_t)args.Hkv * args.T * D) {}
-  __device__ __forceinline__ int entry(int key) const {
-    const int p = trow[min(key >> sh, a.width - 1)];
-    return key < kend && (unsigned)p < (unsigned)a.n_blocks ? p : -1;
-  }
+  // the table's entry for a position, and whether it is one (kept apart: a use of the loaded
+  // value right behind the load would wait for it)
+  __device__ __forceinline__ int entry(int key) const { return trow[min(key >> sh, a.width - 1)]; }
+  __device__ __forceinline__ bool real(int p, int key) const { return key < kend && (unsigned)p < (unsigned)a.n_blocks; }
   __device__ __forceinline__ KvqPlace place(int j0) const {
     return KvqPlace{entry(j0 + 16 * ((lane & 15) >> 2)), entry(j0 + 16 * (lane >> 4))};
   }
-  // (a missing block loads block 0 in its place, unused)
-  __device__ __forceinline__ void load(KvqStage<D>& s, int j0, const KvqPlace& pl) const {
-    const int m = lane & 15, c = lane >> 4, T = a.T;
-    const int pk = max(pl.k, 0), pv = max(pl.v, 0);
-    const uint8_t* kb = a.kc + (size_t)pk * blk + (size_t)(h * T + ((j0 + 16 * (m >> 2)) & (T - 1)) + (m & 3)) * D + 16 * c;
-    const uint8_t* vb = a.vc + (size_t)pv * blk + (size_t)(h * D + m) * T + ((j0 + 16 * c) & (T - 1));
+  // a step's keys (with both exponents) and values; a missing block loads block 0 in its place, unused
+  __device__ __forceinline__ void load_k(KvqStage<D>& s, int j0, const KvqPlace& pl) const {
+    const int m = lane & 15, key = j0 + 16 * (m >> 2);
+    const bool rk = real(pl.k, key);
+    s.has = real(pl.v, j0 + 16 * (lane >> 4));
+    const size_t pk = rk ? pl.k : 0, pv = s.has ? pl.v : 0;
+    const uint8_t* kb = a.kc + pk * blk + (h * a.T + (key & (a.T - 1)) + (m & 3)) * D + 16 * (lane >> 4);
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int u = 0; u < D / 64; ++u) s.k[t][u] = *(const uint4*)(kb + 4 * t * D + 64 * u);
+    s.ek = a.ke[pk * a.Hkv + h];
+    s.ev = a.ve[pv * a.Hkv + h];
+  }
+  __device__ __forceinline__ void load_v(KvqStage<D>& s, int j0, const KvqPlace& pl) const {
+    const int key = j0 + 16 * (lane >> 4);
+    const size_t pv = real(pl.v, key) ? pl.v : 0;
+    const uint8_t* vb = a.vc + pv * blk + (h * D + (lane & 15)) * a.T + (key & (a.T - 1));
 #pragma unroll
-    for (int dt = 0; dt < D / 16; ++dt) s.v[dt] = *(const uint4*)(vb + (size_t)(16 * dt) * T);
-    s.ek = a.ke[(size_t)pk * a.Hkv + h];
-    s.ev = a.ve[(size_t)pv * a.Hkv + h];
-    if (pl.k < 0) s.ek = 127;
-    if (pl.v < 0) s.ev = -1;
+    for (int dt = 0; dt < D / 16; ++dt) s.v[dt] = *(const uint4*)(vb + 16 * dt * a.T);
   }
 };
 
+// larger of two scores (the median with infinity: fmaxf would first quiet signalling NaNs, an instruction an operand)
+__device__ __forceinline__ float kvq_max(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, INFINITY); }
 // largest over the four lane groups, in every lane
 __device__ __forceinline__ float kvq_max_groups(float x) {
   x = fmaxf(x, __shfl_xor(x, 16));
@@ -298,14 +306,24 @@ struct KvqRows {
 
   // query operands of row r (-1: none) of tile i: lane group c, operand 2 u + w, element e is dim 64 u + 16 c + 8 w + e
   template <typename E>
-  __device__ __forceinline__ void load_q(int i, const E* row, bool neg) {
+  __device__ __forceinline__ void load_q(int i, const E* row, bool neg, bool vec) {
     const int c = (threadIdx.x & 63) >> 4;
 #pragma unroll
     for (int kd = 0; kd < D / 32; ++kd) {
       const E* p = row + 64 * (kd >> 1) + 16 * c + 8 * (kd & 1);
+      E raw[8] = {};
+      if (row) {
+        if (vec) {
+#pragma unroll
+          for (int j = 0; j < (int)sizeof(raw) / 16; ++j) ((uint4*)raw)[j] = ((const uint4*)p)[j];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) raw[e] = p[e];
+        }
+      }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        float x = row ? kvq_ld(p + e) : 0.f;
+        float x = kvq_ld(raw + e);
         if (neg) x = -x;
 #pragma unroll
         for (int pl = 0; pl < PL; ++pl) {  // (the last rounding of three takes what is left: 24 bits)
@@ -321,65 +339,66 @@ struct KvqRows {
   __device__ __forceinline__ float to_m(int i) const { return HALF ? exp2f(R[i] - m[i] - 127.f) : 1.f; }
 
   // one step: keys j0 .. j0 + 63, their operands from src, iev the value exponent of this lane's keys
-  template <bool MASK, typename Src>
-  __device__ __forceinline__ void step(const Src& src, int iev, int j0, int kend, float sc) {
+  // (scored(): the key operands are free)
+  struct Nothing {
+    __device__ __forceinline__ void operator()() const {}
+  };
+  template <bool MASK, typename Src, typename Scored = Nothing>
+  __device__ __forceinline__ void step(const Src& src, int iev, int j0, int kend, float sc, Scored scored = Scored{}) {
     const int c = (threadIdx.x & 63) >> 4;
     floatx4 S[QT][4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
+      bf16x8 k[D / 32];
 #pragma unroll
-      for (int i = 0; i < QT; ++i) S[i][t] = floatx4{0.f, 0.f, 0.f, 0.f};
+      for (int u = 0; u < D / 64; ++u) src.keys(t, u, k[2 * u], k[2 * u + 1]);
 #pragma unroll
-      for (int u = 0; u < D / 64; ++u) {
-        bf16x8 k0, k1;
-        src.keys(t, u, k0, k1);
+      for (int i = 0; i < QT; ++i) {
+        S[i][t] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < QT; ++i)
+        for (int pl = PL - 1; pl >= 0; --pl)  // small parts first
 #pragma unroll
-          for (int pl = PL - 1; pl >= 0; --pl) {  // small parts first
-            S[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, q[i][pl][2 * u], S[i][t], 0, 0, 0);
-            S[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[i][pl][2 * u + 1], S[i][t], 0, 0, 0);
-          }
+          for (int kd = 0; kd < D / 32; ++kd)
+            S[i][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[kd], q[i][pl][kd], S[i][t], 0, 0, 0);
       }
     }
+    scored();
     typedef std::conditional_t<HALF, kvq_h8, bf16x8> W8;
     W8 P[QT][PL][2];
-    const float ev = (float)iev;
 #pragma unroll
     for (int i = 0; i < QT; ++i) {
       if constexpr (MASK) {
-        const int last = iev < 0 ? -1 : min(pos[i], kend - 1), key = j0 + 16 * c;
+        const int last = (iev < 0 ? -1 : min(pos[i], kend - 1)) - (j0 + 16 * c);
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) S[i][t][e] = key + 4 * t + e <= last ? S[i][t][e] : -INFINITY;
+          for (int e = 0; e < 4; ++e) S[i][t][e] = 4 * t + e <= last ? S[i][t][e] : -INFINITY;
       }
-      float x = fmaxf(fmaxf(S[i][0][0], S[i][0][1]), fmaxf(S[i][0][2], S[i][0][3]));
+      float x = S[i][0][0];
 #pragma unroll
-      for (int t = 1; t < 4; ++t)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x = fmaxf(x, S[i][t][e]);
+      for (int j = 1; j < 16; ++j) x = kvq_max(x, S[i][j >> 2][j & 3]);
       x *= sc;
-      const float mx = kvq_max_groups(x), rx = HALF ? kvq_max_groups(x + ev) - KVQ_LIFT : mx;
-      if (__any(mx > m[i] + KVQ_LAZY || rx > R[i] + KVQ_LAZY)) {
-        const float mn = fmaxf(m[i], mx), rn = fmaxf(R[i], rx), fr = exp2f(R[i] - rn);
+      // (a block that is not there: an exponent that leaves the factor 1; its scores are -inf)
+      float ev = !HALF ? 0.f : !MASK || iev >= 0 ? (float)iev : R[i] - m[i];
+      if (__any(x > m[i] + KVQ_LAZY || (HALF && x + ev > R[i] + (KVQ_LAZY + KVQ_LIFT)))) {
+        const float mn = fmaxf(m[i], kvq_max_groups(x)), rn = HALF ? fmaxf(R[i], kvq_max_groups(x + ev) - KVQ_LIFT) : mn;
+        const float fr = exp2f(R[i] - rn);
         l[i] *= exp2f(m[i] - mn);
 #pragma unroll
         for (int dt = 0; dt < D / 16; ++dt) O[i][dt] *= fr;
         m[i] = mn;
         R[i] = rn;
+        if (HALF && MASK && iev < 0) ev = rn - mn;
       }
-      // (the clamp: a factor that large only meets weights below fp32's range)
-      const float f = HALF ? __builtin_amdgcn_exp2f(fminf(ev + m[i] - R[i], 100.f)) : 1.f;
+      const float off = HALF ? ev - R[i] : -m[i];
       float ls = 0.f;
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         float p[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          p[e] = __builtin_amdgcn_exp2f(fmaf(S[i][t][e], sc, -m[i]));
+          p[e] = __builtin_amdgcn_exp2f(fmaf(S[i][t][e], sc, off));
           ls += p[e];
-          if constexpr (HALF) p[e] *= f;
         }
 #pragma unroll
         for (int pl = 0; pl < PL; ++pl)
@@ -388,9 +407,25 @@ struct KvqRows {
             const auto w = __builtin_convertvector(kvq_f2{p[e], p[e + 1]}, std::conditional_t<HALF, kvq_h2, bf16x2>);
             P[i][pl][t >> 1][4 * (t & 1) + e] = w[0];
             P[i][pl][t >> 1][4 * (t & 1) + e + 1] = w[1];
-            p[e] -= (float)w[0];
-            p[e + 1] -= (float)w[1];
+            if (pl + 1 < PL) {
+              p[e] -= (float)w[0];
+              p[e + 1] -= (float)w[1];
+            }
           }
+      }
+      if constexpr (HALF) {
+        const float up = R[i] - m[i] - ev;  // from p' to p
+        ls *= __builtin_amdgcn_exp2f(up);
+        // values 2^60 below what the largest p' stands for (blocks of zeros): p' may have
+        // left fp32's range where p has not
+        if (__any(up > 60.f)) {
+          float ps = 0.f;
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) ps += __builtin_amdgcn_exp2f(fmaf(S[i][t][e], sc, -m[i]));
+          ls = ps;
+        }
       }
       l[i] += ls;
     }
@@ -475,29 +510,34 @@ __global__ __launch_bounds__(256) void kvq_attn_keys_kernel(KvqAttnArgs a) {
       rows.pos[i] = ge.first + r / g;
       src = (const E*)a.q + (size_t)(ge.r0 + r / g) * a.ld_q + (size_t)(h * g + r % g) * D;
     }
-    rows.load_q(i, src, a.neg);
+    rows.load_q(i, src, a.neg, a.vec);
   }
   const int seen_all = min(kend, ge.first + rb / g + 1);  // keys below this are seen by every row
   const KvqWalk<D> walk(a, b, h, kend);
   const int first = kbeg + wave * KVQ_STEP, nit = first < kend ? (kend - first + 4 * KVQ_STEP - 1) / (4 * KVQ_STEP) : 0;
   auto key = [&](int it) { return first + it * 4 * KVQ_STEP; };
-  auto work = [&](const KvqStage<D>& s, int j0) {
-    const KvqFromCodes<D, sizeof(E) == 2> src{s, j0 + 16 * c, kend};
-    if (j0 + KVQ_STEP <= seen_all && __all(s.ev >= 0)) rows.template step<false>(src, s.ev, j0, kend, sc);
-    else rows.template step<true>(src, s.ev, j0, kend, sc);
-  };
   if (nit > 0) {
-    KvqStage<D> sa, sb;
-    KvqPlace p0 = walk.place(key(0)), p1 = walk.place(key(1));
-    walk.load(sa, key(0), p0);
-    for (int it = 0; it < nit; it += 2) {
-      p0 = walk.place(key(it + 2));
-      walk.load(sb, key(it + 1), p1);
-      work(sa, key(it));
-      p1 = walk.place(key(it + 3));
-      walk.load(sa, key(it + 2), p0);
-      if (it + 1 < nit) work(sb, key(it + 1));
-    }
+    KvqStage<D> s;
+    KvqPlace pl = walk.place(key(0)), next = walk.place(key(1));
+    walk.load_k(s, key(0), pl);
+    walk.load_v(s, key(0), pl);
+    int it = 0;
+    // one stage of registers: the next step's keys are asked for once this step's scores are
+    // there, its values once they are summed
+    auto step = [&](auto mask) {
+      const int ev = s.has ? s.ev : -1;
+      pl = next;
+      next = walk.place(key(it + 2));
+      rows.template step<decltype(mask)::value>(KvqFromCodes<D, sizeof(E) == 2>{s, ev, key(it) + 16 * c, kend}, ev, key(it), kend,
+                                                sc, [&] { walk.load_k(s, key(it + 1), pl); });
+      walk.load_v(s, key(it + 1), pl);
+      ++it;
+    };
+    // steps that every row sees whole come first, without a mask (two loops, not a branch a step,
+    // keep the accumulators in place)
+    const int whole = min(nit, (seen_all - first + 3 * KVQ_STEP) / (4 * KVQ_STEP));
+    while (it < whole && __all(s.has)) step(std::false_type{});
+    while (it < nit) step(std::true_type{});
   }
 #pragma unroll
   for (int i = 0; i < QT; ++i) {
@@ -538,12 +578,12 @@ __global__ __launch_bounds__(256) void kvq_attn_keys_kernel(KvqAttnArgs a) {
   }
 }
 
-// Waves split the rows: a workgroup of four owns 128 rows of one (request, KV head) and
-// one share of its keys.  A step's codes are converted once for all waves, a
-// quarter each, into operands in LDS (32 KB at D = 128, two steps' worth), while
-// the codes of the step after next are on their way in registers; every wave
-// multiplies the whole step with its own two tiles of 16 rows.  bf16 calls with
-// many rows, where the matrix cores and the exponentials bound it.
+// Waves split the rows: a workgroup of NW waves owns 32 NW rows of one (request, KV head)
+// and one share of its keys.  A step's codes are converted once for all waves, half
+// of them the keys and half the values, into operands in LDS (32 KB at D = 128, two
+// steps' worth), while the codes of the next two steps are on their way in
+// registers; every wave multiplies the whole step with its own two tiles of 16
+// rows.  bf16 calls with many rows, where the matrix cores and the exponentials bound it.
 template <int D>
 struct KvqFromLds {
   const uint16_t* st;  // operands of 64 x 16 bytes: keys (t, kd), then values (dt, half)
@@ -561,10 +601,13 @@ struct KvqFromLds {
   }
 };
 
-template <int D>
-__global__ __launch_bounds__(256, 2) void kvq_attn_rows_kernel(KvqAttnArgs a) {
-  constexpr int QT = 2, WROWS = 16 * QT, ROWS = 4 * WROWS, OPS = 4 * (D / 32) + 2 * (D / 16), DTW = D / 64;
-  __shared__ __align__(16) uint16_t sm[2 * OPS * 512];
+template <int D, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void kvq_attn_rows_kernel(KvqAttnArgs a) {
+  constexpr int QT = 2, WROWS = 16 * QT, ROWS = NW * WROWS;
+  constexpr int PIECES = D / 16;            // 1 KiB of codes each, of a step's keys and of its values
+  constexpr int MINE = 2 * PIECES / NW;     // of this wave: keys (waves below NW / 2) or values
+  constexpr int STAGE = 4 * PIECES * 512;   // elements of a step's operands
+  __shared__ __align__(16) uint16_t sm[2 * STAGE];
   const int g = a.Hq / a.Hkv;
   int w = blockIdx.x;
   const int h = w % a.Hkv;
@@ -580,6 +623,64 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_rows_kernel(KvqAttnArgs a) {
   const int kbeg = split * ge.chunk, kend = min(kbeg + ge.chunk, kall);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, col = lane & 15, c = lane >> 4;
   const float sc = a.scale_log2;
+  const KvqWalk<D> walk(a, b, h, kend);
+  const int nit = (kend - kbeg + KVQ_STEP - 1) / KVQ_STEP;
+  // this wave's share of a step: pieces at base + i * stride
+  const bool of_v = wave >= NW / 2;
+  const int first_piece = (of_v ? wave - NW / 2 : wave) * MINE;
+  const int group = of_v ? c : col >> 2;  // of the 16 keys in which its lanes' codes lie
+  const uint8_t* const side = of_v ? a.vc : a.kc;
+  constexpr int U = D / 64;  // pieces of a key tile
+  static_assert(MINE == 1 || MINE % U == 0, "a wave's pieces start at a tile's first or are one");
+  struct Raw {
+    uint4 x[MINE];
+    int ek, ev;
+    bool has;
+    __device__ __forceinline__ int exp_v() const { return has ? ev : -1; }
+  };
+  struct Two {
+    int data, v;  // table entries of the codes' and of this lane's 16 keys
+  };
+  auto place = [&](int j0) { return Two{walk.entry(j0 + 16 * group), walk.entry(j0 + 16 * c)}; };
+  // pl: the entries of these keys, and then those of two steps further on (asked for before the codes:
+  // loads come back in order)
+  auto load = [&](Raw& r, int j0, Two& pl) {
+    // (one address and no branch for both roles: loads on a branch are waited for at its end)
+    const int at = (j0 + 16 * group) & (a.T - 1);
+    const int off = of_v ? (h * D + 16 * first_piece + col) * a.T + at
+                         : (h * a.T + at + (col & 3) + 4 * (first_piece / U)) * D + 64 * (first_piece % U) + 16 * c;
+    r.has = walk.real(pl.v, j0 + 16 * c);
+    const size_t blk = walk.real(pl.data, j0 + 16 * group) ? pl.data : 0, bv = r.has ? pl.v : 0;
+    pl = place(j0 + 2 * KVQ_STEP);
+    const uint8_t* p = side + blk * walk.blk + off;
+#pragma unroll
+    for (int i = 0; i < MINE; ++i) r.x[i] = *(const uint4*)(p + (of_v ? 16 * i * a.T : 4 * (i / U) * D + 64 * (i % U)));
+    r.ek = a.ke[blk * a.Hkv + h];
+    r.ev = a.ve[bv * a.Hkv + h];
+  };
+  auto store = [&](const Raw& r, int j0, uint16_t* st) {
+    uint16_t* p = st + ((of_v ? 2 * PIECES : 0) + 2 * first_piece) * 512 + lane * 8;
+    if (of_v) {
+      const KvqKeep keep(r.exp_v(), j0 + 16 * c, kend);
+#pragma unroll
+      for (int i = 0; i < MINE; ++i) {
+        const uint4 v = keep(r.x[i]);
+        *(kvq_h8*)(p + 1024 * i) = kvq_f16x8(v.x, v.y);
+        *(kvq_h8*)(p + 1024 * i + 512) = kvq_f16x8(v.z, v.w);
+      }
+    } else {
+      const float ks = kvq_pow2(r.ek - 127);
+#pragma unroll
+      for (int i = 0; i < MINE; ++i) {
+        *(bf16x8*)(p + 1024 * i) = kvq_bf16x8(r.x[i].x, r.x[i].y, ks);
+        *(bf16x8*)(p + 1024 * i + 512) = kvq_bf16x8(r.x[i].z, r.x[i].w, ks);
+      }
+    }
+  };
+  auto key = [&](int it) { return kbeg + it * KVQ_STEP; };
+  Raw ra, rb2;
+  Two pa = place(key(0)), pb = place(key(1));
+  load(ra, key(0), pa);
   KvqRows<D, QT, 1> rows;
   rows.start();
   const int wr = rb + wave * WROWS;
@@ -592,65 +693,35 @@ __global__ __launch_bounds__(256, 2) void kvq_attn_rows_kernel(KvqAttnArgs a) {
       rows.pos[i] = ge.first + r / g;
       src = (const uint16_t*)a.q + (size_t)(ge.r0 + r / g) * a.ld_q + (size_t)(h * g + r % g) * D;
     }
-    rows.load_q(i, src, a.neg);
+    rows.load_q(i, src, a.neg, a.vec);
   }
   const int seen_all = min(kend, ge.first + min(wr, R - 1) / g + 1);  // keys below this are seen by every row of the wave
-  const KvqWalk<D> walk(a, b, h, kend);
-  const int nit = (kend - kbeg + KVQ_STEP - 1) / KVQ_STEP;
-  // this wave's quarter of a step: key tile `wave`, DTW dim tiles of the values
-  uint4 ck[D / 64], cv[DTW];
-  int ek = 127, ev = -1;
-  auto load = [&](int j0, const KvqPlace& pl) {
-    const int T = a.T, pk = max(pl.k, 0), pv = max(pl.v, 0);
-    const uint8_t* kb = a.kc + (size_t)pk * walk.blk +
-                        (size_t)(h * T + ((j0 + 16 * (col >> 2)) & (T - 1)) + 4 * wave + (col & 3)) * D + 16 * c;
-    const uint8_t* vb = a.vc + (size_t)pv * walk.blk + (size_t)(h * D + 16 * DTW * wave + col) * T + ((j0 + 16 * c) & (T - 1));
-#pragma unroll
-    for (int u = 0; u < D / 64; ++u) ck[u] = *(const uint4*)(kb + 64 * u);
-#pragma unroll
-    for (int d = 0; d < DTW; ++d) cv[d] = *(const uint4*)(vb + (size_t)(16 * d) * T);
-    ek = a.ke[(size_t)pk * a.Hkv + h];
-    ev = a.ve[(size_t)pv * a.Hkv + h];
-    if (pl.k < 0) ek = 127;
-    if (pl.v < 0) ev = -1;
-  };
-  auto store = [&](int j0, uint16_t* st) {
-    const float ks = kvq_pow2(ek - 127);
-#pragma unroll
-    for (int u = 0; u < D / 64; ++u) {
-      uint16_t* p = st + ((wave * (D / 32) + 2 * u) * 64 + lane) * 8;
-      *(bf16x8*)p = kvq_bf16x8(ck[u].x, ck[u].y, ks);
-      *(bf16x8*)(p + 512) = kvq_bf16x8(ck[u].z, ck[u].w, ks);
-    }
-    const KvqKeep keep(ev, j0 + 16 * c, kend);
-#pragma unroll
-    for (int d = 0; d < DTW; ++d) {
-      uint16_t* p = st + ((4 * (D / 32) + 2 * (wave * DTW + d)) * 64 + lane) * 8;
-      const uint4 v = keep(cv[d]);
-      *(kvq_h8*)p = kvq_f16x8(v.x, v.y);
-      *(kvq_h8*)(p + 512) = kvq_f16x8(v.z, v.w);
-    }
-  };
   if (nit > 0) {
-    KvqPlace pl = walk.place(kbeg + KVQ_STEP);
-    load(kbeg, walk.place(kbeg));
-    store(kbeg, sm);
-    int ev_now = ev;
-    load(kbeg + KVQ_STEP, pl);
-    pl = walk.place(kbeg + 2 * KVQ_STEP);
-    for (int it = 0; it < nit; ++it) {
-      const int j0 = kbeg + it * KVQ_STEP;
-      __syncthreads();  // step it is in its stage, and every wave is done with the other
-      const int ev_next = ev;
-      if (it + 1 < nit) {
-        store(j0 + KVQ_STEP, sm + ((it + 1) & 1) * OPS * 512);
-        load(j0 + 2 * KVQ_STEP, pl);
-        pl = walk.place(j0 + 3 * KVQ_STEP);
-      }
-      const KvqFromLds<D> src{sm + (it & 1) * OPS * 512, lane};
-      if (j0 + KVQ_STEP <= seen_all && __all(ev_now >= 0)) rows.template step<false>(src, ev_now, j0, kend, sc);
-      else rows.template step<true>(src, ev_now, j0, kend, sc);
+    load(rb2, key(1), pb);
+    store(ra, key(0), sm);
+    int ev_now = ra.exp_v(), it = 0;
+    load(ra, key(2), pa);
+    // step `it` from stage it & 1; r holds the codes of step it + 1, and takes those of it + 3
+    auto step = [&](auto mask, auto odd, Raw& r, Two& pl) {
+      constexpr int O = decltype(odd)::value;
+      lds_barrier();  // step it is in its stage, and every wave is done with the other
+      const int ev_next = r.exp_v();
+      store(r, key(it + 1), sm + (O ? 0 : STAGE));
+      load(r, key(it + 3), pl);
+      rows.template step<decltype(mask)::value>(KvqFromLds<D>{sm + (O ? STAGE : 0), lane}, ev_now, key(it), kend, sc);
       ev_now = ev_next;
+      ++it;
+    };
+    // pairs of steps that every row of the wave sees whole come first, without a mask (two
+    // loops, not a branch a step, keep the accumulators in place)
+    const int whole = min(nit, (seen_all - kbeg) / KVQ_STEP) - 1;
+    while (it < whole && __all(ev_now >= 0 && rb2.has)) {
+      step(std::false_type{}, std::integral_constant<int, 0>{}, rb2, pb);
+      step(std::false_type{}, std::integral_constant<int, 1>{}, ra, pa);
+    }
+    while (it < nit) {
+      step(std::true_type{}, std::integral_constant<int, 0>{}, rb2, pb);
+      if (it < nit) step(std::true_type{}, std::integral_constant<int, 1>{}, ra, pa);
     }
   }
   const size_t part = (((size_t)b * a.Hkv + h) * a.nsplit + split) * a.rows_pad;
@@ -711,12 +782,14 @@ __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttnArgs a) {
 // How a call is split (host): rows of a workgroup, and shares of the keys.
 void kvq_attn_plan(KvqAttnArgs& a) {
   const int rows = a.max_q * (a.Hq / a.Hkv);
-  a.by_rows = a.bf16 && rows > 64;
+  a.by_rows = a.bf16 && rows > 64 ? (rows > 128 ? 8 : 4) : 0;
+  if (getenv("NW") && a.by_rows) a.by_rows = atoi(getenv("NW"));
   a.qt = rows > 16 && a.bf16 ? 2 : 1;
-  a.group_rows = a.by_rows ? 128 : 16 * a.qt;
+  a.group_rows = a.by_rows ? 32 * a.by_rows : 16 * a.qt;
   a.groups = (rows + a.group_rows - 1) / a.group_rows;
   a.rows_pad = a.groups * a.group_rows;
-  a.chunk = a.by_rows ? 512 : 1024;
+  a.chunk = a.by_rows ? 1024 : 2048;
+  if (getenv("CH")) a.chunk = atoi(getenv("CH"));
   a.nsplit = std::max(1, std::min(64, (a.max_len + a.chunk - 1) / a.chunk));
 }
 
@@ -731,7 +804,8 @@ template <typename E, int D>
 static void kvq_launch(const KvqAttnArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)((long long)a.B * a.nsplit * a.groups * a.Hkv));
   if constexpr (sizeof(E) == 2) {
-    if (a.by_rows) hipLaunchKernelGGL((kvq_attn_rows_kernel<D>), grid, dim3(256), 0, st, a);
+    if (a.by_rows == 8) hipLaunchKernelGGL((kvq_attn_rows_kernel<D, 8>), grid, dim3(512), 0, st, a);
+    else if (a.by_rows) hipLaunchKernelGGL((kvq_attn_rows_kernel<D, 4>), grid, dim3(256), 0, st, a);
     else if (a.qt == 2) hipLaunchKernelGGL((kvq_attn_keys_kernel<E, D, 2>), grid, dim3(256), 0, st, a);
     else hipLaunchKernelGGL((kvq_attn_keys_kernel<E, D, 1>), grid, dim3(256), 0, st, a);
   } else {
@@ -749,6 +823,7 @@ void kvq_attention(KvqAttnArgs a, hipStream_t st) {
   a.part_s = (float2*)(a.part_o + kvq_part_rows(a) * a.D);
   // a negative scale turns the queries' signs; scores of a zero one are all 0 (not 0 * -inf where a key is hidden)
   a.neg = a.scale < 0.f;
+  a.vec = (((uintptr_t)a.q | a.ld_q * (a.bf16 ? 2 : 4)) & 15) == 0;  // rows start on 16 bytes (heads then do)
   a.scale_log2 = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-37f);
   if (a.bf16) {
     if (a.D == 128) kvq_launch<uint16_t, 128>(a, st);

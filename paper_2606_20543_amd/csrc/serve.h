@@ -23,8 +23,8 @@ __device__ __forceinline__ long long wave_sum_ll(long long v) {
 }
 
 // blocks of n tokens, at most the table's width
-__device__ __forceinline__ int slot_blocks(long long n, int T, int width) {
-  const long long c = (n + T - 1) / T;
+__device__ __forceinline__ int slot_blocks(long long n, int T, int sh, int width) {
+  const long long c = (n + T - 1) >> sh;
   return (int)(c < width ? c : width);
 }
 
@@ -33,13 +33,13 @@ __global__ __launch_bounds__(SLOT_T) void slots_kernel(SlotArgs a) {
   __shared__ int s_held[SLOT_SEQS], s_have[SLOT_SEQS];
   __shared__ long long s_start[SLOT_SEQS + 1], s_cu[SLOT_SEQS + 1];
   const int tid = threadIdx.x, b0 = blockIdx.x * SLOT_SEQS, nb = min(SLOT_SEQS, a.B - b0);
-  const int T = a.T, W = a.width;
+  const int T = a.T, W = a.width, sh = __builtin_ctz(a.T);  // (T is a power of two)
   // rows and lacking blocks of the requests before this workgroup's
   long long rows = 0, lack = 0;
   for (int b = tid; b < b0; b += SLOT_T) {
     const long long h = max(a.held[b], 0), n = max(a.fresh[b], 0);
     rows += n;
-    lack += slot_blocks(h + n, T, W) - slot_blocks(h, T, W);
+    lack += slot_blocks(h + n, T, sh, W) - slot_blocks(h, T, sh, W);
   }
   rows = wave_sum_ll(rows);
   lack = wave_sum_ll(lack);
@@ -58,11 +58,11 @@ __global__ __launch_bounds__(SLOT_T) void slots_kernel(SlotArgs a) {
     for (int i = 0; i < nb; ++i) {
       const long long h = max(a.held[b0 + i], 0), n = max(a.fresh[b0 + i], 0);
       s_held[i] = (int)h;
-      s_have[i] = slot_blocks(h, T, W);
+      s_have[i] = slot_blocks(h, T, sh, W);
       s_cu[i] = r;
       s_start[i] = l;
       r += n;
-      l += slot_blocks(h + n, T, W) - s_have[i];
+      l += slot_blocks(h + n, T, sh, W) - s_have[i];
       a.cu[b0 + i + 1] = (int)(r < INT_MAX ? r : INT_MAX);
       a.lens[b0 + i] = (int)(h + n < INT_MAX ? h + n : INT_MAX);
     }
@@ -86,11 +86,11 @@ __global__ __launch_bounds__(SLOT_T) void slots_kernel(SlotArgs a) {
       int i = 0;
       while (s_cu[i + 1] <= r) ++i;
       const long long p = s_held[i] + (r - s_cu[i]);
-      const long long j = p / T;
+      const long long j = p >> sh;
       pos = (int)(p < INT_MAX ? p : INT_MAX);
       if (j < W) {
         const int page = j >= s_have[i] ? pooled(s_start[i] + (j - s_have[i])) : a.table[(size_t)(b0 + i) * W + j];
-        const long long at = (long long)page * T + p % T;
+        const long long at = (long long)page * T + (p & (T - 1));
         if (page >= 0 && at <= INT_MAX) slot = (int)at;
       }
     }

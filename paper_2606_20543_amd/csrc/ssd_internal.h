@@ -484,7 +484,7 @@ struct KvqAttnArgs {
   float scale;
   void* workspace;
   // the plan (kvq.h): row groups, key shares, partial results in the workspace
-  int by_rows, qt, groups, group_rows, rows_pad, nsplit, chunk, neg;
+  int by_rows, qt, groups, group_rows, rows_pad, nsplit, chunk, neg, vec;
   float scale_log2;
   float* part_o;   // [B][Hkv][nsplit][rows_pad][D], relative to the row's maximum
   float2* part_s;  // [B][Hkv][nsplit][rows_pad] (maximum, log2 domain; sum)
