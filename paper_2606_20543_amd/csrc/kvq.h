@@ -304,35 +304,42 @@ struct KvqRows {
     }
   }
 
-  // query operands of row r (-1: none) of tile i: lane group c, operand 2 u + w, element e is dim 64 u + 16 c + 8 w + e
+  // query operands of tile i from a row of q (live: the tile's row is one; else zeros): lane group c,
+  // operand 2 u + w, element e is dim 64 u + 16 c + 8 w + e.  The loads stand on no branch of a lane:
+  // they would be waited for one by one.
   template <typename E>
-  __device__ __forceinline__ void load_q(int i, const E* row, bool neg, bool vec) {
+  __device__ __forceinline__ void load_q(int i, const E* row, bool live, bool neg, bool vec) {
     const int c = (threadIdx.x & 63) >> 4;
+    E raw[D / 32][8];
+    if (vec) {
 #pragma unroll
-    for (int kd = 0; kd < D / 32; ++kd) {
-      const E* p = row + 64 * (kd >> 1) + 16 * c + 8 * (kd & 1);
-      E raw[8] = {};
-      if (row) {
-        if (vec) {
+      for (int kd = 0; kd < D / 32; ++kd)
 #pragma unroll
-          for (int j = 0; j < (int)sizeof(raw) / 16; ++j) ((uint4*)raw)[j] = ((const uint4*)p)[j];
-        } else {
+        for (int j = 0; j < (int)sizeof(E) / 2; ++j)
+          *(uint4*)(raw[kd] + j * (16 / sizeof(E))) = *(const uint4*)(row + 64 * (kd >> 1) + 16 * c + 8 * (kd & 1) + j * (16 / sizeof(E)));
+    } else {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) raw[e] = p[e];
-        }
-      }
+      for (int kd = 0; kd < D / 32; ++kd)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) raw[kd][e] = row[64 * (kd >> 1) + 16 * c + 8 * (kd & 1) + e];
+    }
+#pragma unroll
+    for (int kd = 0; kd < D / 32; ++kd)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        float x = kvq_ld(raw + e);
-        if (neg) x = -x;
+        if constexpr (HALF) {
+          q[i][0][kd][e] = __builtin_bit_cast(__bf16, (uint16_t)(live ? raw[kd][e] ^ (neg ? 0x8000 : 0) : 0));
+        } else {
+          float x = live ? raw[kd][e] : 0.f;
+          if (neg) x = -x;
 #pragma unroll
-        for (int pl = 0; pl < PL; ++pl) {  // (the last rounding of three takes what is left: 24 bits)
-          const uint16_t b = f2bf(x);
-          q[i][pl][kd][e] = __builtin_bit_cast(__bf16, b);
-          x -= bf2f(b);
+          for (int pl = 0; pl < PL; ++pl) {  // (the last rounding of three takes what is left: 24 bits)
+            const uint16_t b = f2bf(x);
+            q[i][pl][kd][e] = __builtin_bit_cast(__bf16, b);
+            x -= bf2f(b);
+          }
         }
       }
-    }
   }
 
   // what takes the sums from R (and the codes' exponents) to m
@@ -504,13 +511,10 @@ __global__ __launch_bounds__(256) void kvq_attn_keys_kernel(KvqAttnArgs a) {
 #pragma unroll
   for (int i = 0; i < QT; ++i) {
     const int r = rb + 16 * i + col;
-    const E* src = nullptr;
-    rows.pos[i] = -1;
-    if (r < R && ge.has(r / g)) {
-      rows.pos[i] = ge.first + r / g;
-      src = (const E*)a.q + (size_t)(ge.r0 + r / g) * a.ld_q + (size_t)(h * g + r % g) * D;
-    }
-    rows.load_q(i, src, a.neg, a.vec);
+    const bool live = r < R && ge.has(r / g);
+    rows.pos[i] = live ? ge.first + r / g : -1;
+    const size_t row = live ? ge.r0 + r / g : 0;
+    rows.load_q(i, (const E*)a.q + row * a.ld_q + (size_t)(h * g + r % g) * D, live, a.neg, a.vec);
   }
   const int seen_all = min(kend, ge.first + rb / g + 1);  // keys below this are seen by every row
   const KvqWalk<D> walk(a, b, h, kend);
@@ -687,13 +691,10 @@ __global__ __launch_bounds__(64 * NW, 2) void kvq_attn_rows_kernel(KvqAttnArgs a
 #pragma unroll
   for (int i = 0; i < QT; ++i) {
     const int r = wr + 16 * i + col;
-    const uint16_t* src = nullptr;
-    rows.pos[i] = -1;
-    if (r < R && ge.has(r / g)) {
-      rows.pos[i] = ge.first + r / g;
-      src = (const uint16_t*)a.q + (size_t)(ge.r0 + r / g) * a.ld_q + (size_t)(h * g + r % g) * D;
-    }
-    rows.load_q(i, src, a.neg, a.vec);
+    const bool live = r < R && ge.has(r / g);
+    rows.pos[i] = live ? ge.first + r / g : -1;
+    const size_t row = live ? ge.r0 + r / g : 0;
+    rows.load_q(i, (const uint16_t*)a.q + row * a.ld_q + (size_t)(h * g + r % g) * D, live, a.neg, a.vec);
   }
   const int seen_all = min(kend, ge.first + min(wr, R - 1) / g + 1);  // keys below this are seen by every row of the wave
   if (nit > 0) {
