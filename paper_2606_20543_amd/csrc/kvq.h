@@ -70,26 +70,110 @@ __device__ __forceinline__ void kvq_store4(float* p, floatx4 o, float l) {
 }
 __device__ __forceinline__ void kvq_store4(uint16_t* p, floatx4 o, float l) {
   const float f = l > 0.f ? 1.f / l : 0.f;
+  const uint32_t x = cvt2bf(o[0] * f, o[1] * f), y = cvt2bf(o[2] * f, o[3] * f);
+  p[0] = (uint16_t)x, p[1] = (uint16_t)(x >> 16), p[2] = (uint16_t)y, p[3] = (uint16_t)(y >> 16);
+}
+
+// N neighbouring elements, read by one load where ALIGNED
+template <typename E, int N, bool ALIGNED>
+struct alignas(ALIGNED ? sizeof(E) * N : sizeof(E)) KvqVec {
+  E v[N];
+};
+
+// largest finite magnitude of n rows of D elements, in every lane: 16 bytes a lane and load where
+// the rows allow it (VEC), else two elements
+template <typename E, bool VEC>
+__device__ __forceinline__ float kvq_amax(const E* src, size_t ld, int n, int D, int lane) {
+  constexpr int N = VEC ? 16 / (int)sizeof(E) : 2, U = 8;  // U loads in flight (rows past the last: that one again)
+  typedef KvqVec<E, N, VEC> V;
+  const int per = D / N, step = 64 / per, c = (lane % per) * N;
+  float m = 0.f;
+  for (int r = lane / per; r < n; r += U * step) {
+    V x[U];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) p[e] = f2bf(o[e] * f);
+    for (int u = 0; u < U; ++u) x[u] = *(const V*)(src + (size_t)min(r + u * step, n - 1) * ld + c);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int e = 0; e < N; ++e) m = fmaxf(m, kvq_mag(kvq_ld(&x[u].v[e])));
+  }
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  return m;
+}
+
+// codes times f (a power of two), rounded again, where keep has ones
+__device__ __forceinline__ uint32_t kvq_again(uint32_t codes, float f, uint32_t keep) {
+  float v[4];
+  kvq_value4(codes, v);
+  return (kvq_code4(v[0] * f, v[1] * f, v[2] * f, v[3] * f) & keep) | (codes & ~keep);
+}
+__device__ __forceinline__ uint32_t kvq_low_bytes(int n) { return n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1u; }
+
+// rows [0, n) of src to tokens off .. of a block's keys [T][D]
+template <typename E, bool VEC>
+__device__ __forceinline__ void kvq_put_keys(const E* src, size_t ld, int n, int D, int off, float inv, uint8_t* blk, int lane) {
+  constexpr int N = VEC ? 16 / (int)sizeof(E) : 2, U = 8;
+  typedef KvqVec<E, N, VEC> V;
+  const int per = D / N, step = 64 / per, c = (lane % per) * N;
+  for (int r = lane / per; r < n; r += U * step) {
+    V x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = *(const V*)(src + (size_t)min(r + u * step, n - 1) * ld + c);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (r + u * step >= n) break;
+      uint8_t* p = blk + (size_t)(off + r + u * step) * D + c;
+      float y[N];
+#pragma unroll
+      for (int e = 0; e < N; ++e) y[e] = kvq_fit(kvq_ld(&x[u].v[e]), inv);
+      if constexpr (N == 2) {
+        *(uint16_t*)p = (uint16_t)kvq_code4(y[0], y[1], 0.f, 0.f);
+      } else {
+#pragma unroll
+        for (int e = 0; e < N; e += 4) *(uint32_t*)(p + e) = kvq_code4(y[e], y[e + 1], y[e + 2], y[e + 3]);
+      }
+    }
+  }
+}
+
+// the same for values [D][T]: a lane owns two neighbouring dims and takes 16 tokens at a time, which
+// are 16 bytes of a dim's row where the run covers them all
+template <typename E, bool VEC>
+__device__ __forceinline__ void kvq_put_values(const E* src, size_t ld, int n, int D, int T, int off, float inv, uint8_t* blk,
+                                               int lane) {
+  typedef KvqVec<E, 2, VEC> V;
+  const int per = D / 2, d = (lane % per) * 2, groups = 64 / per;
+  for (int t0 = (off & ~15) + 16 * (lane / per); t0 < off + n; t0 += 16 * groups) {
+    V x[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) x[j] = *(const V*)(src + (size_t)min(max(t0 + j - off, 0), n - 1) * ld + d);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      uint8_t* p = blk + (size_t)(d + e) * T + t0;
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        w[i] = kvq_code4(kvq_fit(kvq_ld(&x[4 * i].v[e]), inv), kvq_fit(kvq_ld(&x[4 * i + 1].v[e]), inv),
+                         kvq_fit(kvq_ld(&x[4 * i + 2].v[e]), inv), kvq_fit(kvq_ld(&x[4 * i + 3].v[e]), inv));
+      if (t0 >= off && t0 + 16 <= off + n) {
+        *(uint4*)p = make_uint4(w[0], w[1], w[2], w[3]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          if (t0 + j >= off && t0 + j < off + n) p[j] = (uint8_t)(w[j / 4] >> (8 * (j % 4)));
+      }
+    }
+  }
 }
 
 template <typename E>
-__global__ __launch_bounds__(256) void kvq_append_kernel(KvqAppendArgs a) {
-  const int lane = threadIdx.x & 63;
-  const long long task = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int which = (int)(task & 1), h = (int)((task >> 1) % a.Hkv);
-  const long long row = (task >> 1) / a.Hkv;
-  if (row >= a.n_rows) return;
-  const int T = a.T, D = a.D, cap = a.n_blocks * T;
-  const int slot = a.slots[row];
-  if (slot < 0 || slot >= cap) return;
-  const int off = slot % T, page = slot / T;
-  if (row > 0 && off != 0 && a.slots[row - 1] == slot - 1) return;
+__device__ __forceinline__ void kvq_append_run(const KvqAppendArgs& a, int which, int h, int row, int slot, int lane) {
+  const int T = a.T, D = a.D, off = slot & (T - 1), page = slot / T;
   // length of the run
   int n = 0;
   while (true) {
-    const bool in = row + n + lane < a.n_rows && off + n + lane < T && a.slots[row + n + lane] == slot + n + lane;
+    const int r = row + n + lane;
+    const bool in = r < a.n_rows && off + n + lane < T && a.slots[min(r, a.n_rows - 1)] == slot + n + lane;
     const uint64_t m = ~__ballot(in);
     if (m) {
       n += __builtin_ctzll(m);
@@ -97,39 +181,67 @@ __global__ __launch_bounds__(256) void kvq_append_kernel(KvqAppendArgs a) {
     }
     n += 64;
   }
-  const E* src = (const E*)(which ? a.v : a.k) + (size_t)row * (which ? a.ld_v : a.ld_k) + (size_t)h * D;
   const size_t ld = which ? a.ld_v : a.ld_k;
+  const E* src = (const E*)(which ? a.v : a.k) + (size_t)row * ld + (size_t)h * D;
+  const bool vec = which ? a.vec_v : a.vec_k;  // 16-byte loads
   uint8_t* blk = (which ? a.vc : a.kc) + ((size_t)page * a.Hkv + h) * ((size_t)T * D);
   uint8_t* ep = (which ? a.ve : a.ke) + (size_t)page * a.Hkv + h;
-  float amax = 0.f;
-  for (int i = lane; i < n * D; i += 64) amax = fmaxf(amax, kvq_mag(kvq_ld(src + (size_t)(i / D) * ld + i % D)));
-  for (int o = 32; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
-  int s = kvq_exponent(amax);
-  if (off > 0) {
-    const int old = *ep;
-    if (old >= s) {
-      s = old;
+  const int old = off > 0 ? *ep : 0;
+  const float amax = vec ? kvq_amax<E, true>(src, ld, n, D, lane) : kvq_amax<E, false>(src, ld, n, D, lane);
+  const int s = max(kvq_exponent(amax), old);
+  if (off > 0 && s > old) {
+    // 2^(old - s): a factor below every code's smallest part leaves zero
+    const float f = old - s < -126 ? 0.f : kvq_pow2(old - s);
+    if (which) {
+      const int words = (off + 3) / 4;
+      for (int i = lane; i < words * D; i += 64) {
+        uint32_t* p = (uint32_t*)(blk + (size_t)(i / words) * T) + i % words;
+        *p = kvq_again(*p, f, kvq_low_bytes(off - 4 * (i % words)));
+      }
     } else {
-      // 2^(old - s): a factor below every code's smallest part leaves zero
-      const float f = old - s < -126 ? 0.f : kvq_pow2(old - s);
-      for (int i = lane; i < off * D; i += 64) {
-        uint8_t* p = which ? blk + (size_t)(i / off) * T + i % off : blk + i;
-        const float x = __builtin_amdgcn_cvt_f32_fp8((int)*p, 0) * f;
-        *p = (uint8_t)kvq_code4(x, x, x, x);
+      for (int i = lane; i < off * D / 4; i += 64) {
+        uint32_t* p = (uint32_t*)blk + i;
+        *p = kvq_again(*p, f, ~0u);
       }
     }
   }
   if (lane == 0) *ep = (uint8_t)s;
   const float inv = kvq_pow2(127 - s);
-  for (int i = lane; i < n * D; i += 64) {
-    const int t = i / D, d = i % D;
-    const float x = kvq_fit(kvq_ld(src + (size_t)t * ld + d), inv);
-    (which ? blk + (size_t)d * T + off + t : blk + (size_t)(off + t) * D + d)[0] = (uint8_t)kvq_code4(x, x, x, x);
+  if (which) {
+    if (vec) kvq_put_values<E, true>(src, ld, n, D, T, off, inv, blk, lane);
+    else kvq_put_values<E, false>(src, ld, n, D, T, off, inv, blk, lane);
+  } else {
+    if (vec) kvq_put_keys<E, true>(src, ld, n, D, off, inv, blk, lane);
+    else kvq_put_keys<E, false>(src, ld, n, D, off, inv, blk, lane);
   }
 }
 
-void kvq_append(const KvqAppendArgs& a, hipStream_t st) {
-  const long long tasks = (long long)a.n_rows * a.Hkv * 2;
+template <typename E>
+__global__ __launch_bounds__(256) void kvq_append_kernel(KvqAppendArgs a) {
+  const int lane = threadIdx.x & 63;
+  const long long task = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int which = (int)(task & 1), h = (int)((task >> 1) % a.Hkv);
+  const long long first = (task >> 1) / a.Hkv * a.window;
+  if (first >= a.n_rows) return;
+  // the runs that start among this wave's rows
+  const int cap = a.n_blocks * a.T, r = (int)min(first + lane, (long long)a.n_rows - 1);
+  const int slot = a.slots[r], prev = r > 0 ? a.slots[r - 1] : -2;
+  const bool starts = lane < a.window && first + lane < a.n_rows && slot >= 0 && slot < cap &&
+                      ((slot & (a.T - 1)) == 0 || prev != slot - 1);
+  for (uint64_t m = __ballot(starts); m; m &= m - 1) {
+    const int l = __builtin_ctzll(m);
+    kvq_append_run<E>(a, which, h, (int)first + l, __builtin_amdgcn_readlane(slot, l), lane);
+  }
+}
+
+void kvq_append(KvqAppendArgs a, hipStream_t st) {
+  const int es = a.bf16 ? 2 : 4;
+  a.vec_k = (((uintptr_t)a.k | a.ld_k * es) & 15) == 0;
+  a.vec_v = (((uintptr_t)a.v | a.ld_v * es) & 15) == 0;
+  // rows that a wave looks at: one while that makes few enough waves (each may start a run: a step
+  // of single tokens), more for long prompts, where one in a block's rows does
+  a.window = std::max(1, std::min(16, a.n_rows / 1024));
+  const long long tasks = (long long)((a.n_rows + a.window - 1) / a.window) * a.Hkv * 2;
   const dim3 grid((unsigned)((tasks + 3) / 4));
   if (a.bf16) hipLaunchKernelGGL(kvq_append_kernel<uint16_t>, grid, dim3(256), 0, st, a);
   else hipLaunchKernelGGL(kvq_append_kernel<float>, grid, dim3(256), 0, st, a);
@@ -304,39 +416,49 @@ struct KvqRows {
     }
   }
 
-  // query operands of tile i from a row of q (live: the tile's row is one; else zeros): lane group c,
-  // operand 2 u + w, element e is dim 64 u + 16 c + 8 w + e.  The loads stand on no branch of a lane:
-  // they would be waited for one by one.
+  // query operands of the tiles from rows of q (live: the row is one; else zeros): lane group c,
+  // operand 2 u + w, element e is dim 64 u + 16 c + 8 w + e.  All loads go out first, and stand on no
+  // branch of a lane: they would be waited for one by one.
   template <typename E>
-  __device__ __forceinline__ void load_q(int i, const E* row, bool live, bool neg, bool vec) {
+  __device__ __forceinline__ void load_q(const E* const (&row)[QT], const bool (&live)[QT], bool neg, bool vec) {
     const int c = (threadIdx.x & 63) >> 4;
-    E raw[D / 32][8];
+    E raw[QT][D / 32][8];
     if (vec) {
 #pragma unroll
-      for (int kd = 0; kd < D / 32; ++kd)
+      for (int i = 0; i < QT; ++i)
 #pragma unroll
-        for (int j = 0; j < (int)sizeof(E) / 2; ++j)
-          *(uint4*)(raw[kd] + j * (16 / sizeof(E))) = *(const uint4*)(row + 64 * (kd >> 1) + 16 * c + 8 * (kd & 1) + j * (16 / sizeof(E)));
+        for (int kd = 0; kd < D / 32; ++kd)
+#pragma unroll
+          for (int j = 0; j < 8; j += 16 / (int)sizeof(E))
+            *(uint4*)(raw[i][kd] + j) = *(const uint4*)(row[i] + 64 * (kd >> 1) + 16 * c + 8 * (kd & 1) + j);
     } else {
 #pragma unroll
-      for (int kd = 0; kd < D / 32; ++kd)
+      for (int i = 0; i < QT; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) raw[kd][e] = row[64 * (kd >> 1) + 16 * c + 8 * (kd & 1) + e];
+        for (int kd = 0; kd < D / 32; ++kd)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) raw[i][kd][e] = row[i][64 * (kd >> 1) + 16 * c + 8 * (kd & 1) + e];
     }
 #pragma unroll
-    for (int kd = 0; kd < D / 32; ++kd)
+    for (int i = 0; i < QT; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int kd = 0; kd < D / 32; ++kd) {
         if constexpr (HALF) {
-          q[i][0][kd][e] = __builtin_bit_cast(__bf16, (uint16_t)(live ? raw[kd][e] ^ (neg ? 0x8000 : 0) : 0));
+          const uint32_t flip = neg ? 0x80008000u : 0u;
+          uint4 x = __builtin_bit_cast(uint4, raw[i][kd]);
+          x = live[i] ? make_uint4(x.x ^ flip, x.y ^ flip, x.z ^ flip, x.w ^ flip) : make_uint4(0, 0, 0, 0);
+          q[i][0][kd] = __builtin_bit_cast(bf16x8, x);
         } else {
-          float x = live ? raw[kd][e] : 0.f;
-          if (neg) x = -x;
 #pragma unroll
-          for (int pl = 0; pl < PL; ++pl) {  // (the last rounding of three takes what is left: 24 bits)
-            const uint16_t b = f2bf(x);
-            q[i][pl][kd][e] = __builtin_bit_cast(__bf16, b);
-            x -= bf2f(b);
+          for (int e = 0; e < 8; ++e) {
+            float x = live[i] ? raw[i][kd][e] : 0.f;
+            if (neg) x = -x;
+#pragma unroll
+            for (int pl = 0; pl < PL; ++pl) {  // (the last rounding of three takes what is left: 24 bits)
+              const uint16_t b = f2bf(x);
+              q[i][pl][kd][e] = __builtin_bit_cast(__bf16, b);
+              x -= bf2f(b);
+            }
           }
         }
       }
@@ -508,13 +630,17 @@ __global__ __launch_bounds__(256) void kvq_attn_keys_kernel(KvqAttnArgs a) {
   const float sc = a.scale_log2;
   KvqRows<D, QT, sizeof(E) == 2 ? 1 : 3> rows;
   rows.start();
+  {
+    const E* row[QT];
+    bool live[QT];
 #pragma unroll
-  for (int i = 0; i < QT; ++i) {
-    const int r = rb + 16 * i + col;
-    const bool live = r < R && ge.has(r / g);
-    rows.pos[i] = live ? ge.first + r / g : -1;
-    const size_t row = live ? ge.r0 + r / g : 0;
-    rows.load_q(i, (const E*)a.q + row * a.ld_q + (size_t)(h * g + r % g) * D, live, a.neg, a.vec);
+    for (int i = 0; i < QT; ++i) {
+      const int r = rb + 16 * i + col, n = r / g;
+      live[i] = r < R && ge.has(n);
+      rows.pos[i] = live[i] ? ge.first + n : -1;
+      row[i] = (const E*)a.q + (live[i] ? (size_t)(ge.r0 + n) : 0) * a.ld_q + (size_t)(h * g + (r - n * g)) * D;
+    }
+    rows.load_q(row, live, a.neg, a.vec);
   }
   const int seen_all = min(kend, ge.first + rb / g + 1);  // keys below this are seen by every row
   const KvqWalk<D> walk(a, b, h, kend);
@@ -685,16 +811,21 @@ __global__ __launch_bounds__(64 * NW, 2) void kvq_attn_rows_kernel(KvqAttnArgs a
   Raw ra, rb2;
   Two pa = place(key(0)), pb = place(key(1));
   load(ra, key(0), pa);
+  if (NW == 8 && wave < NW / 2) __builtin_amdgcn_s_setprio(1);
   KvqRows<D, QT, 1> rows;
   rows.start();
   const int wr = rb + wave * WROWS;
+  {
+    const uint16_t* row[QT];
+    bool live[QT];
 #pragma unroll
-  for (int i = 0; i < QT; ++i) {
-    const int r = wr + 16 * i + col;
-    const bool live = r < R && ge.has(r / g);
-    rows.pos[i] = live ? ge.first + r / g : -1;
-    const size_t row = live ? ge.r0 + r / g : 0;
-    rows.load_q(i, (const uint16_t*)a.q + row * a.ld_q + (size_t)(h * g + r % g) * D, live, a.neg, a.vec);
+    for (int i = 0; i < QT; ++i) {
+      const int r = wr + 16 * i + col, n = r / g;
+      live[i] = r < R && ge.has(n);
+      rows.pos[i] = live[i] ? ge.first + n : -1;
+      row[i] = (const uint16_t*)a.q + (live[i] ? (size_t)(ge.r0 + n) : 0) * a.ld_q + (size_t)(h * g + (r - n * g)) * D;
+    }
+    rows.load_q(row, live, a.neg, a.vec);
   }
   const int seen_all = min(kend, ge.first + min(wr, R - 1) / g + 1);  // keys below this are seen by every row of the wave
   if (nit > 0) {
@@ -746,38 +877,44 @@ __global__ __launch_bounds__(64 * NW, 2) void kvq_attn_rows_kernel(KvqAttnArgs a
   }
 }
 
-// Joins the splits of rows that have more than one: a wave a row and query head.
+// Joins the splits of rows that have more than one: D / 4 lanes a row and query head,
+// four splits' loads in flight together.  Bound by the bytes of the partial sums.
 template <typename E, int D>
 __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttnArgs a) {
-  const int g = a.Hq / a.Hkv, lane = threadIdx.x & 63;
-  const long long w = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int r = (int)(w % (a.max_q * g)), h = (int)(w / (a.max_q * g) % a.Hkv), b = (int)(w / (a.max_q * g) / a.Hkv);
+  constexpr int LANES = D / 4;
+  const int g = a.Hq / a.Hkv, rows = a.max_q * g, d = 4 * (threadIdx.x % LANES);
+  const unsigned w = blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+  const int r = (int)(w % rows), h = (int)(w / rows % a.Hkv), b = (int)(w / rows / a.Hkv);
   if (b >= a.B) return;
   const KvqGeom ge(a, b);
   if (r >= ge.n * g || !ge.has(r / g)) return;
   const int kall = ge.keys(r / a.group_rows * a.group_rows, a.group_rows, g), active = (kall + ge.chunk - 1) / ge.chunk;
   if (active <= 1) return;
   const size_t part = ((size_t)b * a.Hkv + h) * a.nsplit * a.rows_pad + r;
-  float M = -INFINITY;
-  for (int s = lane; s < active; s += 64) M = fmaxf(M, a.part_s[part + (size_t)s * a.rows_pad].x);
-  for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
-  constexpr int N = D / 64;
-  float acc[N] = {}, L = 0.f;
-  for (int s = 0; s < active; ++s) {
-    const float2 st = a.part_s[part + (size_t)s * a.rows_pad];
-    const float e = exp2f(st.x - M);
-    L += st.y * e;
-    const float* p = a.part_o + (part + (size_t)s * a.rows_pad) * D + lane * N;
+  float M = KVQ_NONE, L = 0.f;
+  floatx4 o = floatx4{0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < active; s += 4) {
+    float2 st[4];
+    floatx4 v[4];
 #pragma unroll
-    for (int j = 0; j < N; ++j) acc[j] = fmaf(p[j], e, acc[j]);
-  }
-  const float inv = L > 0.f ? 1.f / L : 0.f;
-  E* dst = (E*)a.o + (size_t)(ge.r0 + r / g) * a.ld_o + (size_t)(h * g + r % g) * D + lane * N;
+    for (int j = 0; j < 4; ++j) {  // (past the last: that one again, without weight)
+      const size_t at = part + (size_t)min(s + j, active - 1) * a.rows_pad;
+      st[j] = a.part_s[at];
+      v[j] = *(const floatx4*)(a.part_o + at * D + d);
+    }
+    const float m = fmaxf(M, fmaxf(fmaxf(st[0].x, st[1].x), fmaxf(st[2].x, st[3].x)));
+    const float f = exp2f(M - m);
+    L *= f;
+    o *= f;
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
-    if constexpr (sizeof(E) == 2) dst[j] = f2bf(acc[j] * inv);
-    else dst[j] = acc[j] * inv;
+    for (int j = 0; j < 4; ++j) {
+      const float e = s + j < active ? exp2f(st[j].x - m) : 0.f;
+      L = fmaf(st[j].y, e, L);
+      o += v[j] * e;
+    }
+    M = m;
   }
+  kvq_store4((E*)a.o + (size_t)(ge.r0 + r / g) * a.ld_o + (size_t)(h * g + r % g) * D + d, o, L);
 }
 
 // How a call is split (host): rows of a workgroup, and shares of the keys.
@@ -789,7 +926,12 @@ void kvq_attn_plan(KvqAttnArgs& a) {
   a.group_rows = a.by_rows ? 32 * a.by_rows : 16 * a.qt;
   a.groups = (rows + a.group_rows - 1) / a.group_rows;
   a.rows_pad = a.groups * a.group_rows;
-  a.chunk = a.by_rows ? 1024 : 2048;
+  const long long base = (long long)a.B * a.Hkv * a.groups;
+  auto share = [&](long long n) {  // keys of a share when the longest context has n of them, whole steps
+    n = std::max<long long>(n, 1);
+    return (int)((((long long)a.max_len + n - 1) / n + KVQ_STEP - 1) / KVQ_STEP * KVQ_STEP);
+  };
+  a.chunk = a.by_rows ? std::max(256, share(384 / base)) : 2048;
   if (getenv("CH")) a.chunk = atoi(getenv("CH"));
   a.nsplit = std::max(1, std::min(64, (a.max_len + a.chunk - 1) / a.chunk));
 }
@@ -814,7 +956,7 @@ static void kvq_launch(const KvqAttnArgs& a, hipStream_t st) {
   }
   if (a.nsplit > 1) {
     const long long rows = (long long)a.B * a.Hkv * a.max_q * (a.Hq / a.Hkv);
-    hipLaunchKernelGGL((kvq_merge_kernel<E, D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((kvq_merge_kernel<E, D>), dim3((unsigned)((rows * (D / 4) + 255) / 256)), dim3(256), 0, st, a);
   }
 }
 

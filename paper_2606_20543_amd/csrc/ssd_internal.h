@@ -471,8 +471,9 @@ struct KvqAppendArgs {
   const int* slots;
   const void *k, *v;
   size_t ld_k, ld_v;
+  int vec_k, vec_v, window;  // the plan (kvq.h)
 };
-void kvq_append(const KvqAppendArgs& a, hipStream_t st);
+void kvq_append(KvqAppendArgs a, hipStream_t st);
 struct KvqAttnArgs {
   const uint8_t *kc, *vc, *ke, *ve;
   int n_blocks, T, Hkv, D;
