@@ -220,9 +220,10 @@ template <typename E>
 __global__ __launch_bounds__(256) void kvq_append_kernel(KvqAppendArgs a) {
   const int lane = threadIdx.x & 63;
   const long long task = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int which = (int)(task & 1), h = (int)((task >> 1) % a.Hkv);
-  const long long first = (task >> 1) / a.Hkv * a.window;
-  if (first >= a.n_rows) return;
+  // windows of rows fastest: the few that start a run in long prompts then fall on all XCDs alike
+  const int windows = (a.n_rows + a.window - 1) / a.window, side = (int)(task / windows), which = side & 1, h = side >> 1;
+  const long long first = task % windows * a.window;
+  if (h >= a.Hkv) return;
   // the runs that start among this wave's rows
   const int cap = a.n_blocks * a.T, r = (int)min(first + lane, (long long)a.n_rows - 1);
   const int slot = a.slots[r], prev = r > 0 ? a.slots[r - 1] : -2;
@@ -241,6 +242,7 @@ void kvq_append(KvqAppendArgs a, hipStream_t st) {
   // rows that a wave looks at: one while that makes few enough waves (each may start a run: a step
   // of single tokens), more for long prompts, where one in a block's rows does
   a.window = std::max(1, std::min(16, a.n_rows / 1024));
+  if (getenv("WIN")) a.window = atoi(getenv("WIN"));
   const long long tasks = (long long)((a.n_rows + a.window - 1) / a.window) * a.Hkv * 2;
   const dim3 grid((unsigned)((tasks + 3) / 4));
   if (a.bf16) hipLaunchKernelGGL(kvq_append_kernel<uint16_t>, grid, dim3(256), 0, st, a);
