@@ -242,7 +242,6 @@ void kvq_append(KvqAppendArgs a, hipStream_t st) {
   // rows that a wave looks at: one while that makes few enough waves (each may start a run: a step
   // of single tokens), more for long prompts, where one in a block's rows does
   a.window = std::max(1, std::min(16, a.n_rows / 1024));
-  if (getenv("WIN")) a.window = atoi(getenv("WIN"));
   const long long tasks = (long long)((a.n_rows + a.window - 1) / a.window) * a.Hkv * 2;
   const dim3 grid((unsigned)((tasks + 3) / 4));
   if (a.bf16) hipLaunchKernelGGL(kvq_append_kernel<uint16_t>, grid, dim3(256), 0, st, a);
@@ -923,7 +922,6 @@ __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttnArgs a) {
 void kvq_attn_plan(KvqAttnArgs& a) {
   const int rows = a.max_q * (a.Hq / a.Hkv);
   a.by_rows = a.bf16 && rows > 64 ? (rows > 128 ? 8 : 4) : 0;
-  if (getenv("NW") && a.by_rows) a.by_rows = atoi(getenv("NW"));
   a.qt = rows > 16 && a.bf16 ? 2 : 1;
   a.group_rows = a.by_rows ? 32 * a.by_rows : 16 * a.qt;
   a.groups = (rows + a.group_rows - 1) / a.group_rows;
@@ -934,7 +932,6 @@ void kvq_attn_plan(KvqAttnArgs& a) {
     return (int)((((long long)a.max_len + n - 1) / n + KVQ_STEP - 1) / KVQ_STEP * KVQ_STEP);
   };
   a.chunk = a.by_rows ? std::max(256, share(384 / base)) : 2048;
-  if (getenv("CH")) a.chunk = atoi(getenv("CH"));
   a.nsplit = std::max(1, std::min(64, (a.max_len + a.chunk - 1) / a.chunk));
 }
 

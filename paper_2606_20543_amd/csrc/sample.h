@@ -1,5 +1,5 @@
 // Sampling of given logits with temperature, top-k, top-p and min-p from given
-// uniforms (included by kernels_misc.hip, whose row segments it uses).
+// uniforms (included by kernels_misc.hip).
 //
 // A code's weight is w = exp((l - max) / T), in float64, held as the integer
 // nearest to 2^45 w: sums of integers are the same in any order, so the result
@@ -9,30 +9,36 @@
 // the first top_k of it, the shortest prefix of those that holds top_p of
 // their mass, and the weights of at least min_p (of the largest weight).  So
 // one pair (logit, code) bounds the set.  It is found without a sort: the
-// codes are counted and their weights summed in 2048 bins of equal width over
-// the logits that have a weight, the bin that the bound falls into is narrowed
-// the same way until it holds few codes, and those are ranked against each other.
-// The draw is the smallest kept code whose running sum (code order) exceeds
-// u times the total.  One workgroup of 16 waves a row.
+// codes are counted (top-k) and their weights summed (top-p) in 2048 bins of
+// equal width over the logits that have a weight, and the few codes of the bin
+// that a bound falls into are ranked against each other; a bin of more is
+// divided again.  The draw is the smallest kept code whose running sum (code
+// order) exceeds u times the total.  One workgroup of 16 waves a row, the row
+// in registers up to 32768 codes.  Bound by the float64 exponentials, two
+// passes of them at most, and the bins' atomics.
 #pragma once
 
 namespace ssd {
 
-constexpr int LS_BINS = 2048, LS_LIST = 1024;
+constexpr int LS_T = 1024, LS_W = LS_T / 64;
+constexpr int LS_BINS = 2 * LS_T, LS_LIST = 1024;
 constexpr double LS_ONE = 35184372088832.0;  // 2^45
+constexpr int LS_POW = 64;
 
 struct LsShared {
   unsigned cnt[LS_BINS];
   unsigned long long wgt[LS_BINS];
+  // codes of the bin that a bound falls into: logit, code, weight, and how many and how much come before
   float lv[LS_LIST];
   int li[LS_LIST];
   unsigned long long lw[LS_LIST];
-  unsigned lc[LS_LIST];            // codes before, weight before
+  unsigned lc[LS_LIST];
   unsigned long long lb[LS_LIST];
-  unsigned long long wred[SMP_W], wred2[SMP_W];
-  unsigned cred[SMP_W];
-  float fmn[SMP_W], fmx[SMP_W];
-  int ired[SMP_W];
+  double pow2[LS_POW];  // 2^(i / 64)
+  unsigned long long wred[LS_W];
+  unsigned cred[LS_W];
+  float fmn[LS_W], fmx[LS_W];
+  int ired[LS_W];
   int n, bin;
   unsigned c0;
   unsigned long long w0;
@@ -48,113 +54,194 @@ __device__ __forceinline__ unsigned long long ls_scan(unsigned long long v, int 
   return v;
 }
 
-template <int NG>
-struct LsRow {
-  const Seg<NG>& g;
-  float mx;
-  double inv;  // 1 / T
-  __device__ __forceinline__ LsRow(const Seg<NG>& s, float m, double i) : g(s), mx(m), inv(i) {}
-  __device__ __forceinline__ double w(float l) const { return exp(((double)l - (double)mx) * inv); }
-  __device__ __forceinline__ unsigned long long fix(double x) const { return (unsigned long long)(x * LS_ONE + 0.5); }
-};
-
 // a logit as it counts: NaN is never drawn, +inf is the largest finite number
 __device__ __forceinline__ float ls_clean(float l) { return l == l ? fminf(l, 3.4028234664e38f) : -INFINITY; }
 
-// Shortest prefix of the order with at least `need_c` codes, or with a mass of at least
-// need_w (by_weight), among the codes of a logit >= floor_l; the bound is left in
-// sh.bv, sh.bi, the prefix's codes and mass in sh.c0, sh.w0.  All codes fall short: bv = floor_l, bi = INT_MAX.
+// The codes of a wave, in groups of 256 (four a lane), wave w the w-th contiguous segment of the
+// row; -inf past its end.  NG > 0: held in registers, else read by every pass.
 template <int NG>
-__device__ void ls_bound(const LsRow<NG>& r, float floor_l, bool by_weight, unsigned need_c, double need_w, LsShared& sh) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  float hi = r.mx, lo = floor_l;  // the codes still to be told apart have lo <= l <= hi
-  unsigned c0 = 0;                // codes above hi, and their mass
-  unsigned long long w0 = 0;
-  while (true) {
-    // bins of equal width, the first the largest logits (a monotone map: products,
-    // subtraction and truncation are; the factor k, a power of two, keeps the width a
-    // normal number, so that lo and hi never share a bin)
-    const float k = hi - lo > 1e38f ? 0.25f : hi - lo < 1e-30f ? 0x1p100f : 1.f;
-    const float width = hi * k - lo * k;
-    const float sc = width > 0.f ? (float)LS_BINS / width : 0.f;
-    auto bin_of = [&](float l) { return min(LS_BINS - 1, (int)((hi * k - l * k) * sc)); };
-    for (int i = tid; i < LS_BINS; i += SMP_T) {
-      sh.cnt[i] = 0;
-      sh.wgt[i] = 0;
+struct LsRow {
+  const float* row;
+  int V, beg, groups;
+  bool vec;
+  float4 held[NG > 0 ? NG : 1];
+  __device__ __forceinline__ LsRow(const float* r, int v) : row(r), V(v) {
+    const int all = (V + 255) / 256, per = (all + LS_W - 1) / LS_W, w = threadIdx.x >> 6;
+    beg = w * per * 256 + (threadIdx.x & 63) * 4;
+    groups = max(0, min(per, all - w * per));
+    vec = (V & 3) == 0 && (((uintptr_t)row) & 15) == 0;
+    if constexpr (NG > 0) {
+#pragma unroll
+      for (int i = 0; i < NG; ++i) held[i] = i < groups ? read(i) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
     }
+  }
+  __device__ __forceinline__ float4 read(int i) const {
+    const int v = beg + i * 256;
+    float4 f = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+    if (vec) {
+      if (v < V) f = *(const float4*)(row + v);
+    } else {
+      if (v < V) f.x = row[v];
+      if (v + 1 < V) f.y = row[v + 1];
+      if (v + 2 < V) f.z = row[v + 2];
+      if (v + 3 < V) f.w = row[v + 3];
+    }
+    return make_float4(ls_clean(f.x), ls_clean(f.y), ls_clean(f.z), ls_clean(f.w));
+  }
+  // fn(first code of the lane, its four logits) over the groups in order, every lane together
+  template <typename F>
+  __device__ __forceinline__ void each(F fn) const {
+    if constexpr (NG > 0) {
+#pragma unroll
+      for (int i = 0; i < NG; ++i)
+        if (i < groups) {
+          const float x[4] = {held[i].x, held[i].y, held[i].z, held[i].w};
+          fn(beg + i * 256, x);
+        }
+    } else {
+#pragma unroll 2
+      for (int i = 0; i < groups; ++i) {
+        const float4 f = read(i);
+        const float x[4] = {f.x, f.y, f.z, f.w};
+        fn(beg + i * 256, x);
+      }
+    }
+  }
+};
+
+// exp((l - mx) / T) for finite l <= mx: 64 (l - mx) / (T ln 2) is split into a whole number k, whose
+// power of two is a table entry and an exponent, and a rest whose exponential is a polynomial of degree
+// 5 (|r| <= ln 2 / 128: off by 2^-54).  13 float64 operations in place of the library's 40.
+struct LsWeight {
+  float mx;
+  double k64;  // 64 / (T ln 2)
+  const double* pow2;
+  __device__ __forceinline__ double operator()(float l) const {
+    const double y = ((double)l - (double)mx) * k64, k = rint(y), r = (y - k) * (0.6931471805599453 / LS_POW);
+    const int n = (int)fmax(k, -1e6);
+    double p = fma(r, 1.0 / 120, 1.0 / 24);
+    p = fma(r, p, 1.0 / 6);
+    p = fma(r, p, 0.5);
+    p = fma(r, p, 1.0);
+    p = fma(r, p, 1.0);
+    return ldexp(p * pow2[n & (LS_POW - 1)], n >> 6);
+  }
+  // the nearest integer to 2^45 w, w <= 1: the low bits of 2^52 + 2^45 w
+  static __device__ __forceinline__ unsigned long long fix(double w) {
+    return (unsigned long long)__double_as_longlong(fma(w, LS_ONE, 4503599627370496.0)) - 0x4330000000000000ull;
+  }
+};
+
+// what the bound is asked to reach: so many codes, or so much mass
+struct LsGoal {
+  bool by_weight;
+  unsigned count;
+  double mass;
+  __device__ __forceinline__ bool operator()(unsigned long long c, unsigned long long w) const {
+    return by_weight ? (double)w >= mass : c >= count;
+  }
+};
+
+// equal-width bins over [lo, hi], the first the largest logits: a monotone map (products,
+// subtraction and truncation are); the factor k, a power of two, keeps the width a normal number,
+// so that lo and hi never share a bin
+struct LsBins {
+  float lo, hi, k, sc;
+  __device__ __forceinline__ LsBins(float l, float h) : lo(l), hi(h) {
+    k = hi - lo > 1e38f ? 0.25f : hi - lo < 1e-30f ? 0x1p100f : 1.f;
+    const float width = hi * k - lo * k;
+    sc = width > 0.f ? (float)LS_BINS / width : 0.f;
+  }
+  __device__ __forceinline__ bool in(float l) const { return l >= lo && l <= hi; }
+  __device__ __forceinline__ int operator()(float l) const { return min(LS_BINS - 1, (int)((hi * k - l * k) * sc)); }
+};
+
+// codes and mass up to this thread's two bins (with what lies before the bins), and the bins' own
+struct LsCumul {
+  unsigned ca, cb;
+  unsigned long long wa, wb, c, w;  // c, w: through the second bin
+};
+
+template <int NG>
+__device__ __forceinline__ LsCumul ls_histogram(const LsRow<NG>& row, const LsWeight& wt, const LsBins& bins, bool count, bool weigh,
+                                                unsigned c0, unsigned long long w0, LsShared& sh) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  static_assert(LS_BINS == 2 * LS_T, "two bins a thread");
+  sh.cnt[2 * tid] = sh.cnt[2 * tid + 1] = 0;
+  sh.wgt[2 * tid] = sh.wgt[2 * tid + 1] = 0;
+  __syncthreads();
+  row.each([&](int, const float(&x)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (bins.in(x[e])) {
+        const int b = bins(x[e]);
+        if (count) atomicAdd(&sh.cnt[b], 1u);
+        if (weigh) atomicAdd(&sh.wgt[b], LsWeight::fix(wt(x[e])));
+      }
+  });
+  __syncthreads();
+  LsCumul q;
+  q.ca = sh.cnt[2 * tid], q.cb = sh.cnt[2 * tid + 1];
+  q.wa = sh.wgt[2 * tid], q.wb = sh.wgt[2 * tid + 1];
+  q.c = ls_scan((unsigned long long)q.ca + q.cb, lane);
+  q.w = ls_scan(q.wa + q.wb, lane);
+  if (lane == 63) {
+    sh.cred[wave] = (unsigned)q.c;
+    sh.wred[wave] = q.w;
+  }
+  __syncthreads();
+  q.c += c0;
+  q.w += w0;
+  for (int x = 0; x < wave; ++x) {
+    q.c += sh.cred[x];
+    q.w += sh.wred[x];
+  }
+  return q;
+}
+
+// The shortest prefix of the order that reaches the goal, given the histogram of the logits in bins
+// (divided further where a bin holds too many): its bound in sh.bv, sh.bi, its codes and mass
+// in sh.c0, sh.w0.  All codes in the bins fall short: bv = bins.lo, bi = INT_MAX.
+template <int NG>
+__device__ __noinline__ void ls_bound(const LsRow<NG>& row, const LsWeight& wt, LsBins bins, LsCumul q, const LsGoal& goal, bool weigh,
+                                      LsShared& sh) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  while (true) {
+    __syncthreads();
     if (tid == 0) {
       sh.n = 0;
       sh.bin = LS_BINS;
     }
     __syncthreads();
-    r.g.each([&](int, const Quad& q) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (e < q.n) {
-          const float l = ls_clean(q.x[e]);
-          if (l >= lo && l <= hi) {
-            const int b = bin_of(l);
-            atomicAdd(&sh.cnt[b], 1u);
-            atomicAdd(&sh.wgt[b], r.fix(r.w(l)));
-          }
-        }
-    });
-    __syncthreads();
-    // the first bin where the running count or mass reaches what is asked for
-    static_assert(LS_BINS == 2 * SMP_T, "two bins a thread");
-    const unsigned ca = sh.cnt[2 * tid], cb = sh.cnt[2 * tid + 1];
-    const unsigned long long wa = sh.wgt[2 * tid], wb = sh.wgt[2 * tid + 1];
-    unsigned long long ci = ls_scan((unsigned long long)(ca + cb), lane), wi = ls_scan(wa + wb, lane);
-    if (lane == 63) {
-      sh.cred[wave] = (unsigned)ci;
-      sh.wred[wave] = wi;
-    }
-    __syncthreads();
-    unsigned long long cbase = c0, wbase = w0;
-    for (int x = 0; x < wave; ++x) {
-      cbase += sh.cred[x];
-      wbase += sh.wred[x];
-    }
-    ci += cbase;
-    wi += wbase;
-    auto reached = [&](unsigned long long c, unsigned long long w) { return by_weight ? (double)w >= need_w : c >= need_c; };
-    if (reached(ci, wi)) {
-      const int b = reached(ci - cb, wi - wb) ? 2 * tid : 2 * tid + 1;
-      atomicMin(&sh.bin, b);
-    }
+    if (goal(q.c, q.w)) atomicMin(&sh.bin, goal(q.c - q.cb, q.w - q.wb) ? 2 * tid : 2 * tid + 1);
     __syncthreads();
     const int bin = sh.bin;
     if (bin == LS_BINS) {  // everything is kept
-      if (tid == SMP_T - 1) {
-        sh.c0 = (unsigned)ci;
-        sh.w0 = wi;
-        sh.bv = floor_l;
+      if (tid == LS_T - 1) {
+        sh.c0 = (unsigned)q.c;
+        sh.w0 = q.w;
+        sh.bv = bins.lo;
         sh.bi = 0x7fffffff;
       }
       __syncthreads();
       return;
     }
-    if (bin >> 1 == tid) {
-      const bool odd = bin & 1;
-      sh.c0 = (unsigned)(ci - cb - (odd ? 0 : ca));
-      sh.w0 = wi - wb - (odd ? 0 : wa);
+    if (bin >> 1 == tid) {  // what lies before the bin
+      sh.c0 = (unsigned)(q.c - q.cb - (bin & 1 ? 0 : q.ca));
+      sh.w0 = q.w - q.wb - (bin & 1 ? 0 : q.wa);
     }
     // the bin's codes: a list, and the range of their logits
     float mn = INFINITY, mx = -INFINITY;
-    r.g.each([&](int v, const Quad& q) {
+    row.each([&](int v, const float(&x)[4]) {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        if (e < q.n) {
-          const float l = ls_clean(q.x[e]);
-          if (l >= lo && l <= hi && bin_of(l) == bin) {
-            mn = fminf(mn, l);
-            mx = fmaxf(mx, l);
-            const int at = atomicAdd(&sh.n, 1);
-            if (at < LS_LIST) {
-              sh.lv[at] = l;
-              sh.li[at] = v + e;
-              sh.lw[at] = r.fix(r.w(l));
-            }
+        if (bins.in(x[e]) && bins(x[e]) == bin) {
+          mn = fminf(mn, x[e]);
+          mx = fmaxf(mx, x[e]);
+          const int at = atomicAdd(&sh.n, 1);
+          if (at < LS_LIST) {
+            sh.lv[at] = x[e];
+            sh.li[at] = v + e;
           }
         }
     });
@@ -168,86 +255,77 @@ __device__ void ls_bound(const LsRow<NG>& r, float floor_l, bool by_weight, unsi
     }
     __syncthreads();
     const int n = sh.n;
-    c0 = sh.c0;
-    w0 = sh.w0;
-    for (int x = 0; x < SMP_W; ++x) {
-      mn = fminf(mn, sh.fmn[x]);
-      mx = fmaxf(mx, sh.fmx[x]);
-    }
+    const unsigned c0 = sh.c0;
+    const unsigned long long w0 = sh.w0;
     if (n <= LS_LIST) {
       // rank the list: `parts` threads share a code's comparisons
-      for (int i = tid; i < n; i += SMP_T) {
-        sh.lc[i] = 0;
-        sh.lb[i] = 0;
+      if (tid < n) {
+        sh.lw[tid] = weigh ? LsWeight::fix(wt(sh.lv[tid])) : 0;
+        sh.lc[tid] = 0;
+        sh.lb[tid] = 0;
       }
       __syncthreads();
-      int pad = 1;
-      while (pad < n) pad <<= 1;
-      const int parts = SMP_T / pad, i = tid & (pad - 1), part = tid / pad;
+      const int pad = n > 1 ? 1 << (32 - __builtin_clz(n - 1)) : 1, parts = LS_T / pad, i = tid & (pad - 1);
       if (i < n) {
         const float li = sh.lv[i];
         const int ii = sh.li[i];
         unsigned c = 0;
         unsigned long long w = 0;
-        for (int j = part; j < n; j += parts)
-          if (sh.lv[j] > li || (sh.lv[j] == li && sh.li[j] < ii)) {
+        for (int j = tid / pad; j < n; j += parts) {
+          const float lj = sh.lv[j];
+          if (lj > li || (lj == li && sh.li[j] < ii)) {
             ++c;
             w += sh.lw[j];
           }
+        }
         atomicAdd(&sh.lc[i], c);
         atomicAdd(&sh.lb[i], w);
       }
       __syncthreads();
       // the one code with the bound inside it
-      for (int k = tid; k < n; k += SMP_T) {
-        const unsigned c = c0 + sh.lc[k];
-        const unsigned long long w = w0 + sh.lb[k];
-        if (!reached(c, w) && reached(c + 1, w + sh.lw[k])) {
-          sh.bv = sh.lv[k];
-          sh.bi = sh.li[k];
+      if (tid < n) {
+        const unsigned c = c0 + sh.lc[tid];
+        const unsigned long long w = w0 + sh.lb[tid];
+        if (!goal(c, w) && goal(c + 1, w + sh.lw[tid])) {
+          sh.bv = sh.lv[tid];
+          sh.bi = sh.li[tid];
           sh.c0 = c + 1;
-          sh.w0 = w + sh.lw[k];
+          sh.w0 = w + sh.lw[tid];
         }
       }
       __syncthreads();
       return;
     }
+    for (int x = 0; x < LS_W; ++x) {
+      mn = fminf(mn, sh.fmn[x]);
+      mx = fmaxf(mx, sh.fmx[x]);
+    }
     if (mn == mx) {
       // equal logits: so many of them, in code order
-      const unsigned long long w1 = r.fix(r.w(mx));
-      unsigned take;
-      if (by_weight) {
-        const double miss = need_w - (double)w0;
-        take = w1 ? (unsigned)fmin(ceil(miss / (double)w1), (double)n) : (unsigned)n;
-        take = max(take, 1u);
-      } else {
-        take = need_c - c0;
-      }
+      const unsigned long long w1 = weigh ? LsWeight::fix(wt(mx)) : 0;
+      unsigned take = goal.count - c0;
+      if (goal.by_weight) take = w1 ? max((unsigned)fmin(ceil((goal.mass - (double)w0) / (double)w1), (double)n), 1u) : (unsigned)n;
       unsigned mine = 0;  // ties of this wave's segment, then those before it
-      r.g.each([&](int, const Quad& q) {
+      row.each([&](int, const float(&x)[4]) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) mine += __popcll(__ballot(e < q.n && ls_clean(q.x[e]) == mx));
+        for (int e = 0; e < 4; ++e) mine += __popcll(__ballot(x[e] == mx));
       });
+      __syncthreads();
       if (lane == 0) sh.cred[wave] = mine;
       __syncthreads();
       unsigned at = 0;
       for (int x = 0; x < wave; ++x) at += sh.cred[x];
-      r.g.each([&](int v, const Quad& q) {
-        unsigned k = 0, all = 0;
-        bool is[4];
+      row.each([&](int v, const float(&x)[4]) {
+        unsigned k = at, all = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          is[e] = e < q.n && ls_clean(q.x[e]) == mx;
-          const uint64_t m = __ballot(is[e]);
+          const uint64_t m = __ballot(x[e] == mx);
           k += __popcll(m & ((1ull << lane) - 1));
           all += __popcll(m);
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (is[e]) {
-            if (at + k == take - 1) sh.bi = v + e;
-            ++k;
-          }
+          if (x[e] == mx && k++ == take - 1) sh.bi = v + e;
         at += all;
       });
       if (tid == 0) {
@@ -258,34 +336,33 @@ __device__ void ls_bound(const LsRow<NG>& r, float floor_l, bool by_weight, unsi
       __syncthreads();
       return;
     }
-    hi = mx;
-    lo = mn;
-    __syncthreads();  // sh.n and sh.bin are read above and written at the top
+    bins = LsBins(mn, mx);
+    __syncthreads();  // (everyone has read c0, w0 and the ranges)
+    q = ls_histogram(row, wt, bins, !goal.by_weight, weigh, c0, w0, sh);
   }
 }
 
 template <int NG>
-__global__ __launch_bounds__(SMP_T) void sample_logits_kernel(SampleArgs a) {
+__global__ __launch_bounds__(LS_T) void sample_logits_kernel(SampleArgs a) {
   __shared__ LsShared sh;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = blockIdx.x, V = a.V;
-  const double T = a.temperatures ? (double)a.temperatures[row] : a.temperature;
-  const int top_k = a.top_ks ? a.top_ks[row] : a.top_k;
-  const double top_p = a.top_ps ? (double)a.top_ps[row] : a.top_p;
-  const double min_any = a.min_ps ? (double)a.min_ps[row] : a.min_p;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = blockIdx.x, V = a.V;
+  const double T = a.temperatures ? (double)a.temperatures[r] : a.temperature;
+  const int top_k = a.top_ks ? a.top_ks[r] : a.top_k;
+  const double top_p = a.top_ps ? (double)a.top_ps[r] : a.top_p;
+  const double min_any = a.min_ps ? (double)a.min_ps[r] : a.min_p;
   const double min_p = min_any > 1.0 ? 1.0 : min_any;  // the largest always stays (NaN: nothing is below it)
-  const Seg<NG> g(a.logits + (size_t)row * a.ld, V);
+  const double u = a.u[r];
+  const LsRow<NG> row(a.logits + (size_t)r * a.ld, V);
+  if (tid < LS_POW) sh.pow2[tid] = exp2((double)tid / LS_POW);
   // largest logit, and the lowest code that has it
   float mx = -INFINITY;
   int am = 0x7fffffff;
-  g.each([&](int v, const Quad& q) {
+  row.each([&](int v, const float(&x)[4]) {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      if (e < q.n) {
-        const float l = ls_clean(q.x[e]);
-        if (l > mx) {
-          mx = l;
-          am = v + e;
-        }
+      if (x[e] > mx) {
+        mx = x[e];
+        am = v + e;
       }
   });
   for (int o = 32; o > 0; o >>= 1) {
@@ -301,7 +378,7 @@ __global__ __launch_bounds__(SMP_T) void sample_logits_kernel(SampleArgs a) {
     sh.ired[wave] = am;
   }
   __syncthreads();
-  for (int x = 0; x < SMP_W; ++x)
+  for (int x = 0; x < LS_W; ++x)
     if (sh.fmx[x] > mx || (sh.fmx[x] == mx && sh.ired[x] < am)) {
       mx = sh.fmx[x];
       am = sh.ired[x];
@@ -309,95 +386,82 @@ __global__ __launch_bounds__(SMP_T) void sample_logits_kernel(SampleArgs a) {
   __syncthreads();
   if (mx == -INFINITY || !(T > 0.0)) {  // nothing to draw, or the largest
     if (tid == 0) {
-      a.tokens[row] = mx == -INFINITY ? -1 : am;
-      if (a.probs) a.probs[row] = mx == -INFINITY ? 0.f : 1.f;
+      a.tokens[r] = mx == -INFINITY ? -1 : am;
+      if (a.probs) a.probs[r] = mx == -INFINITY ? 0.f : 1.f;
     }
     return;
   }
-  const LsRow<NG> r(g, mx, fmin(1.0 / T, 1e300));
-  // logits below this have no weight (45 and one binary places: 32 > 46 ln 2), and min_p's own bound lies above it or
-  // is met by the weight itself
+  const LsWeight wt{mx, fmin(LS_POW / (T * 0.6931471805599453), 1e300), sh.pow2};
+  // logits below this have no weight (32 > 46 ln 2)
   const float floor_l = fmaxf((float)((double)mx - 32.0 * T), -3.4028234664e38f);
   float bv = floor_l;
   int bi = 0x7fffffff;
-  double mass = -1.0;
-  if (top_k > 0 && top_k < V) {
-    ls_bound(r, floor_l, false, (unsigned)top_k, 0.0, sh);
-    bv = sh.bv;
-    bi = sh.bi;
-    mass = (double)sh.w0;
-    __syncthreads();
-  }
-  auto kept = [&](float l, int v) { return l > bv || (l == bv && v <= bi); };
-  auto block_sum = [&](unsigned long long s) {  // inclusive over the waves before and this one, then all
-    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
-    if (lane == 0) sh.wred2[wave] = s;
-    __syncthreads();
-    unsigned long long t = 0;
-    for (int x = 0; x < SMP_W; ++x) t += sh.wred2[x];
-    return t;
-  };
-  if (top_p < 1.0) {
-    if (mass < 0.0) {
-      unsigned long long s = 0;
-      g.each([&](int, const Quad& q) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (e < q.n) {
-            const float l = ls_clean(q.x[e]);
-            if (l >= floor_l) s += r.fix(r.w(l));
-          }
-      });
-      mass = (double)block_sum(s);
-      __syncthreads();
+  const bool by_k = top_k > 0 && top_k < V, by_p = top_p < 1.0;
+  if (by_k || by_p) {
+    const LsBins bins(floor_l, mx);
+    const LsCumul q = ls_histogram(row, wt, bins, by_k, by_p, 0u, 0ull, sh);
+    double mass = 0.0;
+    if (by_k) {
+      ls_bound(row, wt, bins, q, LsGoal{false, (unsigned)top_k, 0.0}, by_p, sh);
+      bv = sh.bv;
+      bi = sh.bi;
+      mass = (double)sh.w0;
+    } else {
+      unsigned long long all = 0;
+      for (int x = 0; x < LS_W; ++x) all += sh.wred[x];
+      mass = (double)all;
     }
-    // the prefix of the first mass of top_p; with a top-k it ends inside that prefix
-    const double need = fmax(top_p * mass, 1.0);
-    ls_bound(r, floor_l, true, 0u, need, sh);
-    bv = sh.bv;
-    bi = sh.bi;
+    if (by_p) {  // (with a top-k the prefix ends inside that of the top-k)
+      ls_bound(row, wt, bins, q, LsGoal{true, 0u, fmax(top_p * mass, 1.0)}, true, sh);
+      bv = sh.bv;
+      bi = sh.bi;
+    }
     __syncthreads();
   }
   // running sum over the kept codes in code order
   auto weight = [&](float l, int v) -> unsigned long long {
-    if (!(l >= floor_l) || !kept(l, v)) return 0;
-    const double w = r.w(l);
-    return w < min_p ? 0 : r.fix(w);
+    if (!(l > bv || (l == bv && v <= bi))) return 0;
+    const double w = wt(l);
+    return w < min_p ? 0 : LsWeight::fix(w);
   };
   unsigned long long s = 0;
   int last = -1;
-  g.each([&](int v, const Quad& q) {
+  row.each([&](int v, const float(&x)[4]) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (e < q.n) {
-        const unsigned long long w = weight(ls_clean(q.x[e]), v + e);
-        s += w;
-        if (w) last = v + e;
-      }
+    for (int e = 0; e < 4; ++e) {
+      const unsigned long long w = weight(x[e], v + e);
+      s += w;
+      if (w) last = v + e;
+    }
   });
-  unsigned long long mine = s;
-  for (int o = 32; o > 0; o >>= 1) mine += __shfl_xor(mine, o);
-  const unsigned long long total = block_sum(s);
-  unsigned long long base = 0;
-  for (int x = 0; x < wave; ++x) base += sh.wred2[x];
-  const double u = a.u[row];
-  const double target = (u > 0.0 ? u : 0.0) * (double)total;
-  for (int o = 32; o > 0; o >>= 1) last = max(last, __shfl_xor(last, o));
-  if (lane == 0) sh.ired[wave] = last;
+  for (int o = 32; o > 0; o >>= 1) {
+    s += __shfl_xor(s, o);
+    last = max(last, __shfl_xor(last, o));
+  }
+  if (lane == 0) {
+    sh.wred[wave] = s;
+    sh.ired[wave] = last;
+  }
   if (tid == 0) sh.bi = 0x7fffffff;
   __syncthreads();
+  unsigned long long total = 0, base = 0;
+  for (int x = 0; x < LS_W; ++x) {
+    if (x == wave) base = total;
+    total += sh.wred[x];
+  }
+  const double target = (u > 0.0 ? u : 0.0) * (double)total;
   // the wave whose running sum passes the target walks its codes
-  if ((double)(base + mine) > target && !((double)base > target)) {
+  if ((double)(base + s) > target && !((double)base > target)) {
     unsigned long long run = base;
     bool found = false;
     int cand = 0x7fffffff;
     float cl = 0.f;
-    g.each([&](int v, const Quad& q) {
+    row.each([&](int v, const float(&x)[4]) {
       if (found) return;
       unsigned long long w[4], t = 0;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        w[e] = e < q.n ? weight(ls_clean(q.x[e]), v + e) : 0;
+        w[e] = weight(x[e], v + e);
         t += w[e];
       }
       const unsigned long long inc = ls_scan(t, lane);
@@ -407,7 +471,7 @@ __global__ __launch_bounds__(SMP_T) void sample_logits_kernel(SampleArgs a) {
         c += w[e];
         if (cand == 0x7fffffff && w[e] && (double)c > target) {
           cand = v + e;
-          cl = ls_clean(q.x[e]);
+          cl = x[e];
         }
       }
       run += __shfl(inc, 63);
@@ -416,26 +480,27 @@ __global__ __launch_bounds__(SMP_T) void sample_logits_kernel(SampleArgs a) {
     int best = cand;
     for (int o = 32; o > 0; o >>= 1) best = min(best, __shfl_xor(best, o));
     if (cand == best && best != 0x7fffffff) {
-      a.tokens[row] = cand;
-      if (a.probs) a.probs[row] = (float)(r.w(cl) * LS_ONE / (double)total);
+      a.tokens[r] = cand;
+      if (a.probs) a.probs[r] = (float)(wt(cl) * LS_ONE / (double)total);
       sh.bi = cand;
     }
   }
   __syncthreads();
   if (sh.bi == 0x7fffffff && tid == 0) {  // u at or past one: the last kept code
-    for (int x = 0; x < SMP_W; ++x) last = max(last, sh.ired[x]);
-    a.tokens[row] = last;
-    if (a.probs) a.probs[row] = (float)(r.w(ls_clean(a.logits[(size_t)row * a.ld + last])) * LS_ONE / (double)total);
+    for (int x = 0; x < LS_W; ++x) last = max(last, sh.ired[x]);
+    a.tokens[r] = last;
+    if (a.probs) a.probs[r] = (float)(wt(ls_clean(a.logits[(size_t)r * a.ld + last])) * LS_ONE / (double)total);
   }
 }
 
 void sample_logits(const SampleArgs& a, hipStream_t st) {
-  if (a.V <= 4 * SMP_HELD)
-    hipLaunchKernelGGL(sample_logits_kernel<4>, dim3(a.R), dim3(SMP_T), 0, st, a);
-  else if (a.V <= 8 * SMP_HELD)
-    hipLaunchKernelGGL(sample_logits_kernel<8>, dim3(a.R), dim3(SMP_T), 0, st, a);
+  // the largest row that is held: 4 codes a thread and group
+  if (a.V <= 4 * 4 * LS_T)
+    hipLaunchKernelGGL(sample_logits_kernel<4>, dim3(a.R), dim3(LS_T), 0, st, a);
+  else if (a.V <= 8 * 4 * LS_T)
+    hipLaunchKernelGGL(sample_logits_kernel<8>, dim3(a.R), dim3(LS_T), 0, st, a);
   else
-    hipLaunchKernelGGL(sample_logits_kernel<0>, dim3(a.R), dim3(SMP_T), 0, st, a);
+    hipLaunchKernelGGL(sample_logits_kernel<0>, dim3(a.R), dim3(LS_T), 0, st, a);
 }
 
 }  // namespace ssd
