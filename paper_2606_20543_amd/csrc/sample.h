@@ -23,7 +23,7 @@ namespace ssd {
 constexpr int LS_T = 1024, LS_W = LS_T / 64;
 constexpr int LS_BINS = 2 * LS_T, LS_LIST = 1024;
 constexpr double LS_ONE = 35184372088832.0;  // 2^45
-constexpr int LS_POW = 64;
+constexpr int LS_POW_LOG2 = 8, LS_POW = 1 << LS_POW_LOG2;
 
 struct LsShared {
   unsigned cnt[LS_BINS];
@@ -34,7 +34,7 @@ struct LsShared {
   unsigned long long lw[LS_LIST];
   unsigned lc[LS_LIST];
   unsigned long long lb[LS_LIST];
-  double pow2[LS_POW];  // 2^(i / 64)
+  double pow2[LS_POW];  // 2^(45 + i / 256)
   unsigned long long wred[LS_W];
   unsigned cred[LS_W];
   float fmn[LS_W], fmx[LS_W];
@@ -64,7 +64,7 @@ struct LsRow {
   const float* row;
   int V, beg, groups;
   bool vec;
-  float4 held[NG > 0 ? NG : 1];
+  mutable float4 held[NG > 0 ? NG : 1];
   __device__ __forceinline__ LsRow(const float* r, int v) : row(r), V(v) {
     const int all = (V + 255) / 256, per = (all + LS_W - 1) / LS_W, w = threadIdx.x >> 6;
     beg = w * per * 256 + (threadIdx.x & 63) * 4;
@@ -95,6 +95,9 @@ struct LsRow {
 #pragma unroll
       for (int i = 0; i < NG; ++i)
         if (i < groups) {
+          // (values that the compiler takes for new ones: what a pass computes of them is computed in that
+          // pass, not ahead of the barriers before it nor kept from an earlier one, which ends in scratch memory)
+          asm volatile("" : "+v"(held[i].x), "+v"(held[i].y), "+v"(held[i].z), "+v"(held[i].w));
           const float x[4] = {held[i].x, held[i].y, held[i].z, held[i].w};
           fn(beg + i * 256, x);
         }
@@ -109,26 +112,27 @@ struct LsRow {
   }
 };
 
-// exp((l - mx) / T) for finite l <= mx: 64 (l - mx) / (T ln 2) is split into a whole number k, whose
-// power of two is a table entry and an exponent, and a rest whose exponential is a polynomial of degree
-// 5 (|r| <= ln 2 / 128: off by 2^-54).  13 float64 operations in place of the library's 40.
+// 2^45 exp((l - mx) / T) for logits that have a weight: y = 256 (l - mx) / (T ln 2) is split into a whole
+// number n (the low bits of 1.5 2^52 + y), whose power of two is a table entry with n / 256 added to its
+// exponent, and a rest whose exponential is a polynomial of degree 4 (|r| <= ln 2 / 512: off by 2^-54).
 struct LsWeight {
   float mx;
-  double k64;  // 64 / (T ln 2)
+  double scale;  // 256 / (T ln 2)
   const double* pow2;
   __device__ __forceinline__ double operator()(float l) const {
-    const double y = ((double)l - (double)mx) * k64, k = rint(y), r = (y - k) * (0.6931471805599453 / LS_POW);
-    const int n = (int)fmax(k, -1e6);
-    double p = fma(r, 1.0 / 120, 1.0 / 24);
-    p = fma(r, p, 1.0 / 6);
+    constexpr double MAGIC = 6755399441055744.0;
+    const double y = ((double)l - (double)mx) * scale, t = y + MAGIC, r = (y - (t - MAGIC)) * (0.6931471805599453 / LS_POW);
+    const int n = (int)(unsigned)__double_as_longlong(t);
+    double p = fma(r, 1.0 / 24, 1.0 / 6);
     p = fma(r, p, 0.5);
     p = fma(r, p, 1.0);
     p = fma(r, p, 1.0);
-    return ldexp(p * pow2[n & (LS_POW - 1)], n >> 6);
+    const long long e = (long long)((unsigned long long)(unsigned)((n >> LS_POW_LOG2) << 20) << 32);
+    return p * __longlong_as_double(__double_as_longlong(pow2[n & (LS_POW - 1)]) + e);
   }
-  // the nearest integer to 2^45 w, w <= 1: the low bits of 2^52 + 2^45 w
+  // the nearest integer to w <= 2^45: the low bits of 2^52 + w
   static __device__ __forceinline__ unsigned long long fix(double w) {
-    return (unsigned long long)__double_as_longlong(fma(w, LS_ONE, 4503599627370496.0)) - 0x4330000000000000ull;
+    return (unsigned long long)__double_as_longlong(w + 4503599627370496.0) - 0x4330000000000000ull;
   }
 };
 
@@ -183,8 +187,13 @@ __device__ __forceinline__ LsCumul ls_histogram(const LsRow<NG>& row, const LsWe
   LsCumul q;
   q.ca = sh.cnt[2 * tid], q.cb = sh.cnt[2 * tid + 1];
   q.wa = sh.wgt[2 * tid], q.wb = sh.wgt[2 * tid + 1];
-  q.c = ls_scan((unsigned long long)q.ca + q.cb, lane);
-  q.w = ls_scan(q.wa + q.wb, lane);
+  unsigned c = q.ca + q.cb;
+  for (int o = 1; o < 64; o <<= 1) {
+    const unsigned t = __shfl_up(c, o);
+    if (lane >= o) c += t;
+  }
+  q.c = c;
+  q.w = weigh ? ls_scan(q.wa + q.wb, lane) : 0;
   if (lane == 63) {
     sh.cred[wave] = (unsigned)q.c;
     sh.wred[wave] = q.w;
@@ -192,9 +201,12 @@ __device__ __forceinline__ LsCumul ls_histogram(const LsRow<NG>& row, const LsWe
   __syncthreads();
   q.c += c0;
   q.w += w0;
-  for (int x = 0; x < wave; ++x) {
-    q.c += sh.cred[x];
-    q.w += sh.wred[x];
+#pragma unroll  // (every wave's read: a loop to its own would wait for each)
+  for (int x = 0; x < LS_W - 1; ++x) {
+    const unsigned cx = sh.cred[x];
+    const unsigned long long wx = sh.wred[x];
+    q.c += x < wave ? cx : 0;
+    q.w += x < wave ? wx : 0;
   }
   return q;
 }
@@ -203,7 +215,7 @@ __device__ __forceinline__ LsCumul ls_histogram(const LsRow<NG>& row, const LsWe
 // (divided further where a bin holds too many): its bound in sh.bv, sh.bi, its codes and mass
 // in sh.c0, sh.w0.  All codes in the bins fall short: bv = bins.lo, bi = INT_MAX.
 template <int NG>
-__device__ __noinline__ void ls_bound(const LsRow<NG>& row, const LsWeight& wt, LsBins bins, LsCumul q, const LsGoal& goal, bool weigh,
+__device__ __forceinline__ void ls_bound(const LsRow<NG>& row, const LsWeight& wt, LsBins bins, LsCumul q, const LsGoal& goal, bool weigh,
                                       LsShared& sh) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   while (true) {
@@ -213,7 +225,8 @@ __device__ __noinline__ void ls_bound(const LsRow<NG>& row, const LsWeight& wt, 
       sh.bin = LS_BINS;
     }
     __syncthreads();
-    if (goal(q.c, q.w)) atomicMin(&sh.bin, goal(q.c - q.cb, q.w - q.wb) ? 2 * tid : 2 * tid + 1);
+    const uint64_t there = __ballot(goal(q.c, q.w));
+    if (there && lane == __builtin_ctzll(there)) atomicMin(&sh.bin, goal(q.c - q.cb, q.w - q.wb) ? 2 * tid : 2 * tid + 1);
     __syncthreads();
     const int bin = sh.bin;
     if (bin == LS_BINS) {  // everything is kept
@@ -296,6 +309,7 @@ __device__ __noinline__ void ls_bound(const LsRow<NG>& row, const LsWeight& wt, 
       __syncthreads();
       return;
     }
+#pragma unroll
     for (int x = 0; x < LS_W; ++x) {
       mn = fminf(mn, sh.fmn[x]);
       mx = fmaxf(mx, sh.fmx[x]);
@@ -314,7 +328,11 @@ __device__ __noinline__ void ls_bound(const LsRow<NG>& row, const LsWeight& wt, 
       if (lane == 0) sh.cred[wave] = mine;
       __syncthreads();
       unsigned at = 0;
-      for (int x = 0; x < wave; ++x) at += sh.cred[x];
+#pragma unroll
+      for (int x = 0; x < LS_W - 1; ++x) {
+        const unsigned cx = sh.cred[x];
+        at += x < wave ? cx : 0;
+      }
       row.each([&](int v, const float(&x)[4]) {
         unsigned k = at, all = 0;
 #pragma unroll
@@ -353,45 +371,33 @@ __global__ __launch_bounds__(LS_T) void sample_logits_kernel(SampleArgs a) {
   const double min_p = min_any > 1.0 ? 1.0 : min_any;  // the largest always stays (NaN: nothing is below it)
   const double u = a.u[r];
   const LsRow<NG> row(a.logits + (size_t)r * a.ld, V);
-  if (tid < LS_POW) sh.pow2[tid] = exp2((double)tid / LS_POW);
-  // largest logit, and the lowest code that has it
+  if (tid < LS_POW) sh.pow2[tid] = LS_ONE * exp2((double)tid / LS_POW);
   float mx = -INFINITY;
-  int am = 0x7fffffff;
-  row.each([&](int v, const float(&x)[4]) {
+  row.each([&](int, const float(&x)[4]) { mx = fmaxf(mx, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]))); });
+  for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+  if (lane == 0) sh.fmx[wave] = mx;
+  __syncthreads();
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (x[e] > mx) {
-        mx = x[e];
-        am = v + e;
-      }
-  });
-  for (int o = 32; o > 0; o >>= 1) {
-    const float m2 = __shfl_xor(mx, o);
-    const int a2 = __shfl_xor(am, o);
-    if (m2 > mx || (m2 == mx && a2 < am)) {
-      mx = m2;
-      am = a2;
-    }
-  }
-  if (lane == 0) {
-    sh.fmx[wave] = mx;
-    sh.ired[wave] = am;
-  }
-  __syncthreads();
-  for (int x = 0; x < LS_W; ++x)
-    if (sh.fmx[x] > mx || (sh.fmx[x] == mx && sh.ired[x] < am)) {
-      mx = sh.fmx[x];
-      am = sh.ired[x];
-    }
-  __syncthreads();
-  if (mx == -INFINITY || !(T > 0.0)) {  // nothing to draw, or the largest
+  for (int x = 0; x < LS_W; ++x) mx = fmaxf(mx, sh.fmx[x]);
+  if (mx == -INFINITY || !(T > 0.0)) {  // nothing to draw, or the largest (its lowest code)
+    int am = 0x7fffffff;
+    row.each([&](int v, const float(&x)[4]) {
+#pragma unroll
+      for (int e = 3; e >= 0; --e)
+        if (x[e] == mx) am = min(am, v + e);
+    });
+    for (int o = 32; o > 0; o >>= 1) am = min(am, __shfl_xor(am, o));
+    if (lane == 0) sh.ired[wave] = am;
+    __syncthreads();
     if (tid == 0) {
+      for (int x = 1; x < LS_W; ++x) am = min(am, sh.ired[x]);
       a.tokens[r] = mx == -INFINITY ? -1 : am;
       if (a.probs) a.probs[r] = mx == -INFINITY ? 0.f : 1.f;
     }
     return;
   }
   const LsWeight wt{mx, fmin(LS_POW / (T * 0.6931471805599453), 1e300), sh.pow2};
+  const double min_w = min_p * LS_ONE;
   // logits below this have no weight (32 > 46 ln 2)
   const float floor_l = fmaxf((float)((double)mx - 32.0 * T), -3.4028234664e38f);
   float bv = floor_l;
@@ -408,6 +414,7 @@ __global__ __launch_bounds__(LS_T) void sample_logits_kernel(SampleArgs a) {
       mass = (double)sh.w0;
     } else {
       unsigned long long all = 0;
+#pragma unroll
       for (int x = 0; x < LS_W; ++x) all += sh.wred[x];
       mass = (double)all;
     }
@@ -422,7 +429,7 @@ __global__ __launch_bounds__(LS_T) void sample_logits_kernel(SampleArgs a) {
   auto weight = [&](float l, int v) -> unsigned long long {
     if (!(l > bv || (l == bv && v <= bi))) return 0;
     const double w = wt(l);
-    return w < min_p ? 0 : LsWeight::fix(w);
+    return w < min_w ? 0 : LsWeight::fix(w);
   };
   unsigned long long s = 0;
   int last = -1;
@@ -445,43 +452,55 @@ __global__ __launch_bounds__(LS_T) void sample_logits_kernel(SampleArgs a) {
   if (tid == 0) sh.bi = 0x7fffffff;
   __syncthreads();
   unsigned long long total = 0, base = 0;
+#pragma unroll
   for (int x = 0; x < LS_W; ++x) {
-    if (x == wave) base = total;
-    total += sh.wred[x];
+    const unsigned long long wx = sh.wred[x];
+    base += x < wave ? wx : 0;
+    total += wx;
   }
   const double target = (u > 0.0 ? u : 0.0) * (double)total;
   // the wave whose running sum passes the target walks its codes
   if ((double)(base + s) > target && !((double)base > target)) {
+    // its groups' sums, the group that passes it, and there the lanes'
     unsigned long long run = base;
+    int at = 0, i = 0;
     bool found = false;
+    row.each([&](int v, const float(&x)[4]) {
+      unsigned long long t = 0;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) t += weight(x[e], v + e);
+      for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o);
+      found |= (double)(run + t) > target;
+      if (!found) {
+        run += t;
+        at = ++i;
+      }
+    });
+    const float4 f = row.read(at);
+    const float x[4] = {f.x, f.y, f.z, f.w};
+    const int v = row.beg + at * 256;
+    unsigned long long w[4], t = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      w[e] = weight(x[e], v + e);
+      t += w[e];
+    }
+    unsigned long long c = run + (ls_scan(t, lane) - t);
     int cand = 0x7fffffff;
     float cl = 0.f;
-    row.each([&](int v, const float(&x)[4]) {
-      if (found) return;
-      unsigned long long w[4], t = 0;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        w[e] = weight(x[e], v + e);
-        t += w[e];
+    for (int e = 0; e < 4; ++e) {
+      c += w[e];
+      if (cand == 0x7fffffff && w[e] && (double)c > target) {
+        cand = v + e;
+        cl = x[e];
       }
-      const unsigned long long inc = ls_scan(t, lane);
-      unsigned long long c = run + (inc - t);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        c += w[e];
-        if (cand == 0x7fffffff && w[e] && (double)c > target) {
-          cand = v + e;
-          cl = x[e];
-        }
-      }
-      run += __shfl(inc, 63);
-      found = __ballot(cand != 0x7fffffff) != 0;
-    });
+    }
     int best = cand;
     for (int o = 32; o > 0; o >>= 1) best = min(best, __shfl_xor(best, o));
     if (cand == best && best != 0x7fffffff) {
       a.tokens[r] = cand;
-      if (a.probs) a.probs[r] = (float)(wt(cl) * LS_ONE / (double)total);
+      if (a.probs) a.probs[r] = (float)(wt(cl) / (double)total);
       sh.bi = cand;
     }
   }
@@ -489,7 +508,7 @@ __global__ __launch_bounds__(LS_T) void sample_logits_kernel(SampleArgs a) {
   if (sh.bi == 0x7fffffff && tid == 0) {  // u at or past one: the last kept code
     for (int x = 0; x < LS_W; ++x) last = max(last, sh.ired[x]);
     a.tokens[r] = last;
-    if (a.probs) a.probs[r] = (float)(wt(ls_clean(a.logits[(size_t)r * a.ld + last])) * LS_ONE / (double)total);
+    if (a.probs) a.probs[r] = (float)(wt(ls_clean(a.logits[(size_t)r * a.ld + last])) / (double)total);
   }
 }
 
