@@ -157,16 +157,16 @@ def lib():
 
 def _ptr(x):
     """Address of an array-like: None, int, numpy array or torch tensor."""
-    if x is None:
-        return None
-    if isinstance(x, int):
-        return ctypes.c_void_p(x)
+    if x is None or type(x) is int:
+        return x
     if hasattr(x, "data_ptr"):
         assert x.is_contiguous(), "tensors passed to libssd must be contiguous"
-        return ctypes.c_void_p(x.data_ptr())
+        return x.data_ptr()
     if hasattr(x, "ctypes"):
         assert x.flags["C_CONTIGUOUS"], "arrays passed to libssd must be C-contiguous"
-        return ctypes.c_void_p(x.ctypes.data)
+        return x.ctypes.data
+    if isinstance(x, int):
+        return int(x)
     raise TypeError(f"cannot take the address of {type(x)}")
 
 

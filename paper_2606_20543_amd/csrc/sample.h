@@ -114,23 +114,22 @@ struct LsRow {
 
 // 2^45 exp((l - mx) / T) for logits that have a weight: y = 256 (l - mx) / (T ln 2) is split into a whole
 // number n (the low bits of 1.5 2^52 + y), whose power of two is a table entry with n / 256 added to its
-// exponent, and a rest whose exponential is a polynomial of degree 4 (|r| <= ln 2 / 512: off by 2^-54).
+// exponent, and a rest f, |f| <= 1/2, whose power 2^(f / 256) is a polynomial of degree 4 (off by 2^-54).
+// (A table of 1024 and degree 3 measured the same.)
 struct LsWeight {
   float mx;
   double scale;  // 256 / (T ln 2)
   const double* pow2;
   __device__ __forceinline__ double operator()(float l) const {
-    constexpr double MAGIC = 6755399441055744.0;
-    const double y = ((double)l - (double)mx) * scale, t = y + MAGIC, r = (y - (t - MAGIC)) * (0.6931471805599453 / LS_POW);
+    constexpr double MAGIC = 6755399441055744.0, C = 0.6931471805599453 / LS_POW;
+    const double y = ((double)l - (double)mx) * scale, t = y + MAGIC, f = y - (t - MAGIC);
     const int n = (int)(unsigned)__double_as_longlong(t);
-    double p = fma(r, 1.0 / 24, 1.0 / 6);
-    p = fma(r, p, 0.5);
-    p = fma(r, p, 1.0);
-    p = fma(r, p, 1.0);
+    const double p = fma(f, fma(f, fma(f, fma(f, C * C * C * C / 24, C * C * C / 6), C * C / 2), C), 1.0);
     const long long e = (long long)((unsigned long long)(unsigned)((n >> LS_POW_LOG2) << 20) << 32);
     return p * __longlong_as_double(__double_as_longlong(pow2[n & (LS_POW - 1)]) + e);
   }
-  // the nearest integer to w <= 2^45: the low bits of 2^52 + w
+  // the nearest integer to w <= 2^45, as a double (a thread's sums stay exact), and from the low bits of 2^52 + w
+  static __device__ __forceinline__ double whole(double w) { return (w + 4503599627370496.0) - 4503599627370496.0; }
   static __device__ __forceinline__ unsigned long long fix(double w) {
     return (unsigned long long)__double_as_longlong(w + 4503599627370496.0) - 0x4330000000000000ull;
   }
@@ -425,30 +424,43 @@ __global__ __launch_bounds__(LS_T) void sample_logits_kernel(SampleArgs a) {
     }
     __syncthreads();
   }
-  // running sum over the kept codes in code order
-  auto weight = [&](float l, int v) -> unsigned long long {
-    if (!(l > bv || (l == bv && v <= bi))) return 0;
+  // The draw: the sums of the kept weights by wave and group (256 codes), the wave and the group
+  // whose running sum passes the target, and there the lane and the code.
+  auto kept = [&](float l, int v) { return l > bv || (l == bv && v <= bi); };
+  auto weight = [&](float l) {  // whole, 0 below min_p
     const double w = wt(l);
-    return w < min_w ? 0 : LsWeight::fix(w);
+    return w < min_w ? 0.0 : LsWeight::whole(w);
   };
-  unsigned long long s = 0;
-  int last = -1;
-  row.each([&](int v, const float(&x)[4]) {
+  auto group_sum = [&](int v, const float(&x)[4], double (&w)[4]) {
+    bool k[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const unsigned long long w = weight(x[e], v + e);
-      s += w;
-      if (w) last = v + e;
+      k[e] = kept(x[e], v + e);
+      w[e] = 0.0;
     }
-  });
-  for (int o = 32; o > 0; o >>= 1) {
-    s += __shfl_xor(s, o);
-    last = max(last, __shfl_xor(last, o));
+    if (__any(k[0] || k[1] || k[2] || k[3])) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const double y = weight(k[e] ? x[e] : bv);
+        w[e] = k[e] ? y : 0.0;
+      }
+    }
+    return (w[0] + w[1]) + (w[2] + w[3]);
+  };
+  double gs[NG > 0 ? NG : 1], s = 0.0;
+  {
+    int i = 0;
+#pragma unroll
+    for (int g = 0; g < (NG > 0 ? NG : 1); ++g) gs[g] = 0.0;
+    row.each([&](int v, const float(&x)[4]) {
+      double w[4];
+      const double t = group_sum(v, x, w);
+      s += t;
+      if constexpr (NG > 0) gs[i++] = t;
+    });
   }
-  if (lane == 0) {
-    sh.wred[wave] = s;
-    sh.ired[wave] = last;
-  }
+  const unsigned long long inc = ls_scan((unsigned long long)s, lane);
+  if (lane == 63) sh.wred[wave] = inc;
   if (tid == 0) sh.bi = 0x7fffffff;
   __syncthreads();
   unsigned long long total = 0, base = 0;
@@ -459,56 +471,67 @@ __global__ __launch_bounds__(LS_T) void sample_logits_kernel(SampleArgs a) {
     total += wx;
   }
   const double target = (u > 0.0 ? u : 0.0) * (double)total;
-  // the wave whose running sum passes the target walks its codes
-  if ((double)(base + s) > target && !((double)base > target)) {
-    // its groups' sums, the group that passes it, and there the lanes'
+  auto draw = [&](int v, float l) {
+    a.tokens[r] = v;
+    if (a.probs) a.probs[r] = (float)(wt(l) / (double)total);
+    sh.bi = v;
+  };
+  if (!((double)base > target) && (double)(base + __shfl(inc, 63)) > target) {
     unsigned long long run = base;
-    int at = 0, i = 0;
+    int at = 0;
     bool found = false;
-    row.each([&](int v, const float(&x)[4]) {
-      unsigned long long t = 0;
+    auto pass = [&](double t) {  // t: a group's sum
+      found |= (double)(run + (unsigned long long)t) > target;
+      run += found ? 0 : (unsigned long long)t;
+      at += found ? 0 : 1;
+    };
+    if constexpr (NG > 0) {
+      for (int o = 32; o > 0; o >>= 1)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) t += weight(x[e], v + e);
-      for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o);
-      found |= (double)(run + t) > target;
-      if (!found) {
-        run += t;
-        at = ++i;
-      }
-    });
+        for (int g = 0; g < NG; ++g) gs[g] += __shfl_xor(gs[g], o);
+#pragma unroll
+      for (int g = 0; g < NG; ++g) pass(gs[g]);
+    } else {
+      row.each([&](int v, const float(&x)[4]) {
+        if (found) return;
+        double w[4], t = group_sum(v, x, w);
+        for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o);
+        pass(t);
+      });
+    }
     const float4 f = row.read(at);
     const float x[4] = {f.x, f.y, f.z, f.w};
     const int v = row.beg + at * 256;
-    unsigned long long w[4], t = 0;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      w[e] = weight(x[e], v + e);
-      t += w[e];
-    }
+    double w[4];
+    const unsigned long long t = (unsigned long long)group_sum(v, x, w);
     unsigned long long c = run + (ls_scan(t, lane) - t);
-    int cand = 0x7fffffff;
-    float cl = 0.f;
+    if (!((double)c > target) && (double)(c + t) > target) {
+      found = false;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      c += w[e];
-      if (cand == 0x7fffffff && w[e] && (double)c > target) {
-        cand = v + e;
-        cl = x[e];
+      for (int e = 0; e < 4; ++e) {
+        c += (unsigned long long)w[e];
+        if (!found && (double)c > target) {
+          found = true;
+          draw(v + e, x[e]);
+        }
       }
-    }
-    int best = cand;
-    for (int o = 32; o > 0; o >>= 1) best = min(best, __shfl_xor(best, o));
-    if (cand == best && best != 0x7fffffff) {
-      a.tokens[r] = cand;
-      if (a.probs) a.probs[r] = (float)(wt(cl) / (double)total);
-      sh.bi = cand;
     }
   }
   __syncthreads();
-  if (sh.bi == 0x7fffffff && tid == 0) {  // u at or past one: the last kept code
-    for (int x = 0; x < LS_W; ++x) last = max(last, sh.ired[x]);
-    a.tokens[r] = last;
-    if (a.probs) a.probs[r] = (float)(wt(ls_clean(a.logits[(size_t)r * a.ld + last])) / (double)total);
+  if (sh.bi == 0x7fffffff) {  // u at or past one: the last code that has a weight
+    int last = -1;
+    row.each([&](int v, const float(&x)[4]) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (kept(x[e], v + e) && weight(x[e]) > 0.0) last = max(last, v + e);
+    });
+    for (int o = 32; o > 0; o >>= 1) last = max(last, __shfl_xor(last, o));
+    if (lane == 0) sh.ired[wave] = last;
+    __syncthreads();
+    if (tid == 0) {
+      for (int x = 0; x < LS_W; ++x) last = max(last, sh.ired[x]);
+      draw(last, ls_clean(a.logits[(size_t)r * a.ld + last]));
+    }
   }
 }
 

@@ -4,11 +4,17 @@
 
 namespace {
 
-// One array argument: `bytes` of device memory of the current device, aligned to
-// its elements.  (ld, rows) arrays end with their last row's last element.
+// The array arguments of one call: each `bytes` of device memory of the current device, whole inside one
+// allocation and aligned to its elements.  Asking the runtime takes 0.4 us an array, as long as a third of a small
+// kernel's launch: an array in an allocation that an earlier one of the same call lies in is not asked for again
+// (small tensors of a caching allocator share one).
 struct ArrayCheck {
-  int dev = -1;
+  int dev = -1, n = 0;
   const char* bad = nullptr;
+  struct {
+    uintptr_t base;
+    size_t size;
+  } seen[4];
   explicit ArrayCheck(void* stream) {
     hipDevice_t sd = -1;
     if (hipGetDevice(&dev) != hipSuccess) {
@@ -24,7 +30,32 @@ struct ArrayCheck {
     }
   }
   void need(const char* name, const void* p, size_t bytes, size_t align) {
-    if (!bad && bytes && !is_local_ptr(p, align, bytes)) bad = name;
+    if (bad || !bytes) return;
+    const uintptr_t at = (uintptr_t)p;
+    if (!p || (at & (align - 1))) {
+      bad = name;
+      return;
+    }
+    for (int i = 0; i < n; ++i)
+      if (at >= seen[i].base && at - seen[i].base < seen[i].size && bytes <= seen[i].size - (at - seen[i].base)) return;
+    hipPointerAttribute_t attr;
+    hipDeviceptr_t base = nullptr;
+    size_t size = 0;
+    if (hipPointerGetAttributes(&attr, p) != hipSuccess || attr.type != hipMemoryTypeDevice || attr.device != dev ||
+        hipMemGetAddressRange(&base, &size, const_cast<void*>(p)) != hipSuccess) {
+      (void)hipGetLastError();
+      bad = name;
+      return;
+    }
+    const size_t off = at - (uintptr_t)base;
+    if (off > size || bytes > size - off) {
+      bad = name;
+      return;
+    }
+    if (n < 4) {
+      seen[n].base = (uintptr_t)base;
+      seen[n++].size = size;
+    }
   }
   ssd_status status() const {
     return bad ? fail(SSD_E_INVAL, "%s: needs an aligned array of the current device, whole inside one allocation", bad)
