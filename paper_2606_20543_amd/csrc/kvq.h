@@ -919,20 +919,43 @@ __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttnArgs a) {
 }
 
 // How a call is split (host): rows of a workgroup, and shares of the keys.
+//
+// Rows of one (request, KV head): up to 64 (and all fp32 calls) take the kernel whose waves split the
+// keys, 16 or 32 rows a workgroup; more the one whose waves split the rows, 256 or 128 rows a
+// workgroup, whichever pads them less (8 x 64 rows of four heads a KV head, contexts to 4352:
+// 46 us against 284 with 32 rows a workgroup).
+//
+// Shares: the least of a cost model of the longest context.  A round (256 keys of a workgroup whose
+// waves split them, 64 where they split the rows) takes 1.4 (1.0 at D = 64) or 1.75 us while the workgroups draw less than
+// the HBM gives, or fit the CUs; more rounds in turn beyond about 200 workgroups (contexts are ragged:
+// not all have their longest).  A second share adds the merge: its launch, and a part for each share.
+// One token at 16000 keys, 8B heads: 15.0 us with 32 shares, 87 with one; 64 requests of up to 8000: 126 with
+// one, 132 to 189 with 2 to 32.
 void kvq_attn_plan(KvqAttnArgs& a) {
   const int rows = a.max_q * (a.Hq / a.Hkv);
-  a.by_rows = a.bf16 && rows > 64 ? (rows > 128 ? 8 : 4) : 0;
+  auto padded = [&](int n) { return (rows + n - 1) / n * n; };
+  a.by_rows = !a.bf16 || rows <= 64 ? 0 : padded(256) * 9LL <= padded(128) * 10LL ? 8 : 4;
   a.qt = rows > 16 && a.bf16 ? 2 : 1;
   a.group_rows = a.by_rows ? 32 * a.by_rows : 16 * a.qt;
   a.groups = (rows + a.group_rows - 1) / a.group_rows;
   a.rows_pad = a.groups * a.group_rows;
-  const long long base = (long long)a.B * a.Hkv * a.groups;
-  auto share = [&](long long n) {  // keys of a share when the longest context has n of them, whole steps
-    n = std::max<long long>(n, 1);
-    return (int)((((long long)a.max_len + n - 1) / n + KVQ_STEP - 1) / KVQ_STEP * KVQ_STEP);
-  };
-  a.chunk = a.by_rows ? std::max(256, share(384 / base)) : 2048;
-  a.nsplit = std::max(1, std::min(64, (a.max_len + a.chunk - 1) / a.chunk));
+  const double base = (double)a.B * a.Hkv * a.groups;
+  const int round = a.by_rows ? KVQ_STEP : 4 * KVQ_STEP;
+  const long long rounds = (a.max_len + round - 1) / round;
+  double best = 0.0;
+  a.nsplit = 1;
+  for (int n = 1; n <= 64 && n <= rounds; ++n) {
+    const long long each = (rounds + n - 1) / n;
+    const double us = each * (a.by_rows ? 1.75 * std::max(1.0, base * n / (a.by_rows == 8 ? 340 : 680))
+                                        : (a.D == 64 ? 1.0 : 1.4) * std::max(1.0, base * n / 200)) +
+                      (n > 1 ? 2.5 + 0.25 * n + base * n * a.group_rows * a.D * 1e-6 : 0.0);
+    if (n == 1 || us < best) {
+      best = us;
+      a.nsplit = n;
+    }
+  }
+  a.chunk = (int)((rounds + a.nsplit - 1) / a.nsplit) * round;
+  a.nsplit = (a.max_len + a.chunk - 1) / a.chunk;
 }
 
 static size_t kvq_part_rows(const KvqAttnArgs& a) { return (size_t)a.B * a.Hkv * a.nsplit * a.rows_pad; }
