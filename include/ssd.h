@@ -604,6 +604,37 @@ typedef struct {
 ssd_status ssd_sample_logits(const ssd_sample_params* params, int32_t R, const float* logits, const float* u,
                              int32_t* tokens, float* probs, void* stream);
 
+/*
+ * The next code of every sequence of a session (image, when guided) from its carry,
+ * by ssd_sample_logits: params as there (vocab and ld are ignored, the carry's are
+ * taken), u [B] fp32, tokens [B] out (vocabulary ids; -1 where nothing can be
+ * drawn), probs [B] fp32 out or NULL; device arrays, on the session's stream.
+ * Changes nothing in the session: the tokens go into the next verify step's block.
+ * (Rules (B) and (C) take temperature and top-k alone, and their own uniforms.)
+ */
+ssd_status ssd_session_sample(ssd_session* sess, const ssd_sample_params* params, const float* u, int32_t* tokens,
+                              float* probs);
+
+/*
+ * Rotary positions with several axes for the positions behind a session's prompt:
+ * sections as in ssd_rope_axes (their sum is head_dim / 2), positions int32
+ * [n_axes][max_ctx - P], entry [a][i] the position on axis a of sequence position
+ * P + i (the same for all sequences: row and column of a grid, say), host or
+ * device.  The prompt keeps its raster positions, which are equal on all axes.
+ * Before anything was committed behind the prompt (SSD_E_STATE otherwise; a second
+ * call replaces the first).  Errors: SSD_E_INVAL for NULL arguments or
+ * bad sections; SSD_E_OOM.
+ */
+ssd_status ssd_session_set_axes(ssd_session* sess, int32_t n_axes, const int32_t* section, const int32_t* positions);
+
+/*
+ * Copy a layer's cached keys (rotated) and values of positions [0, n) of every
+ * sequence, n at most the least frontier: k_out, v_out [B][n][n_kv_heads][head_dim] in
+ * the model's dtype, device arrays, on the session's stream.  The rows are what
+ * ssd_kvq_append takes: a prompt's pass here, its cache there.
+ */
+ssd_status ssd_session_read_kv(ssd_session* sess, int32_t layer, int32_t n, void* k_out, void* v_out);
+
 /* Thread-local description of the last error (empty string if none). */
 const char* ssd_last_error(void);
 

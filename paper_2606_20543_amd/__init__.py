@@ -23,6 +23,7 @@ EXPORTED = [
     "ssd_draft_head_numel", "ssd_draft_head_init", "ssd_draft_head_run", "ssd_free_draft_head",
     "ssd_decode_image_heads", "ssd_plant_image", "ssd_draft_head_run_noalloc",
     "ssd_kvq_slots", "ssd_rope_axes", "ssd_kvq_append", "ssd_kvq_workspace", "ssd_kvq_attention", "ssd_sample_logits",
+    "ssd_session_sample", "ssd_session_set_axes", "ssd_session_read_kv",
 ]
 
 
@@ -145,7 +146,11 @@ def lib():
         L.ssd_kvq_workspace.restype = i64
         L.ssd_kvq_attention.argtypes = [ctypes.POINTER(ssd_kvq_cache), ctypes.POINTER(ssd_kvq_attn_params)] + [vp] * 7
         L.ssd_sample_logits.argtypes = [ctypes.POINTER(ssd_sample_params), i32] + [vp] * 5
-        for name in ("ssd_kvq_slots", "ssd_rope_axes", "ssd_kvq_append", "ssd_kvq_attention", "ssd_sample_logits"):
+        L.ssd_session_sample.argtypes = [vp, ctypes.POINTER(ssd_sample_params), vp, vp, vp]
+        L.ssd_session_set_axes.argtypes = [vp, i32, vp, vp]
+        L.ssd_session_read_kv.argtypes = [vp, i32, i32, vp, vp]
+        for name in ("ssd_kvq_slots", "ssd_rope_axes", "ssd_kvq_append", "ssd_kvq_attention", "ssd_sample_logits",
+                     "ssd_session_sample", "ssd_session_set_axes", "ssd_session_read_kv"):
             getattr(L, name).restype = i32
         for name in ("ssd_init_model", "ssd_prefill", "ssd_verify_step", "ssd_get_carry", "ssd_session_set_cfg",
                      "ssd_decode_image", "ssd_profile", "ssd_profile_read", "ssd_draft_head_init", "ssd_draft_head_run",
@@ -302,6 +307,21 @@ def ssd_kvq_attention(cache, params, q, cu, lens, table, out, workspace=None, st
 def ssd_sample_logits(params, R, logits, u, tokens, probs=None, stream=None):
     _check(lib().ssd_sample_logits(ctypes.byref(params), R, _ptr(logits), _ptr(u), _ptr(tokens), _ptr(probs),
                                    _ptr(stream)))
+
+
+def ssd_session_sample(sess, params, u, tokens, probs=None):
+    """Next codes of a session's sequences from its carry; device arrays [B] (images, when guided)."""
+    _check(lib().ssd_session_sample(ctypes.c_void_p(sess), ctypes.byref(params), _ptr(u), _ptr(tokens), _ptr(probs)))
+
+
+def ssd_session_set_axes(sess, section, positions):
+    """positions int32 [len(section)][max_ctx - P]: axis positions behind the prompt."""
+    sec = (ctypes.c_int32 * max(len(section), 1))(*section)
+    _check(lib().ssd_session_set_axes(ctypes.c_void_p(sess), len(section), sec, _ptr(positions)))
+
+
+def ssd_session_read_kv(sess, layer, n, k_out, v_out):
+    _check(lib().ssd_session_read_kv(ctypes.c_void_p(sess), layer, n, _ptr(k_out), _ptr(v_out)))
 
 
 def ssd_profile(model, enable):

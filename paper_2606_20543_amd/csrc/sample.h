@@ -390,7 +390,7 @@ __global__ __launch_bounds__(LS_T) void sample_logits_kernel(SampleArgs a) {
     __syncthreads();
     if (tid == 0) {
       for (int x = 1; x < LS_W; ++x) am = min(am, sh.ired[x]);
-      a.tokens[r] = mx == -INFINITY ? -1 : am;
+      a.tokens[r] = mx == -INFINITY ? -1 : am + a.add;
       if (a.probs) a.probs[r] = mx == -INFINITY ? 0.f : 1.f;
     }
     return;
@@ -472,7 +472,7 @@ __global__ __launch_bounds__(LS_T) void sample_logits_kernel(SampleArgs a) {
   }
   const double target = (u > 0.0 ? u : 0.0) * (double)total;
   auto draw = [&](int v, float l) {
-    a.tokens[r] = v;
+    a.tokens[r] = v + a.add;
     if (a.probs) a.probs[r] = (float)(wt(l) / (double)total);
     sh.bi = v;
   };

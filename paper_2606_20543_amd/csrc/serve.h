@@ -189,4 +189,57 @@ void rope_axes(const RopeArgs& a, hipStream_t st) {
   }
 }
 
+// the same factors as a session's table, one thread a pair (the float64 formula of rope_table, whose
+// bits equal positions reproduce)
+__global__ __launch_bounds__(256) void rope_axes_table_kernel(RopeTableArgs a) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= (size_t)a.n * a.half) return;
+  const int p = (int)(i / a.half), j = (int)(i - (size_t)p * a.half);
+  int ax = 0, end = a.section[0];
+  while (j >= end) end += a.section[++ax];
+  const double ang = (double)a.pos[(size_t)ax * a.n + p] * pow(a.theta, -(double)j / a.half);
+  a.tab[i] = make_float2((float)cos(ang), (float)sin(ang));
+}
+
+void rope_axes_table(const RopeTableArgs& a, hipStream_t st) {
+  const size_t n = (size_t)a.n * a.half;
+  hipLaunchKernelGGL(rope_axes_table_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, a);
+}
+
+// ---------------- a session's cache as rows ----------------
+// One thread copies eight dims of one position and head: 16 bytes of a key tile, and the value
+// tiles' elements one by one.
+__global__ __launch_bounds__(256) void read_kv_bf16_kernel(int B, int n, int Hkv, int D, int Lmax, const uint16_t* kc,
+                                                           const uint16_t* vc, uint16_t* k, uint16_t* v) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  const int per = D / 8;
+  if (i >= (size_t)B * n * Hkv * per) return;
+  const int c = (int)(i % per), h = (int)(i / per % Hkv), p = (int)(i / ((size_t)per * Hkv) % n);
+  const size_t b = i / ((size_t)per * Hkv * n), base = (b * Hkv + h) * (size_t)Lmax * D;
+  *(uint4*)(k + i * 8) = *(const uint4*)(kc + base + tile16x32_index(p, c * 8, D));
+  uint16_t x[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = vc[base + vtile_index(c * 8 + e, p, Lmax)];
+  *(uint4*)(v + i * 8) = *(const uint4*)x;
+}
+__global__ __launch_bounds__(256) void read_kv_f32_kernel(int B, int n, int Hkv, int D, int Lmax, const float* kc, const float* vc,
+                                                          float* k, float* v) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= (size_t)B * n * Hkv * D) return;
+  const int d = (int)(i % D), h = (int)(i / D % Hkv), p = (int)(i / ((size_t)D * Hkv) % n);
+  const size_t b = i / ((size_t)D * Hkv * n), base = (b * Hkv + h) * (size_t)Lmax * D;
+  k[i] = kc[base + (size_t)p * D + d];
+  v[i] = vc[base + (size_t)d * Lmax + p];
+}
+
+void read_kv(const Dims& dm, int B, int n, int Lmax, const void* kc, const void* vc, void* k, void* v, hipStream_t st) {
+  const size_t all = (size_t)B * n * dm.Hkv * dm.D;
+  if (dm.bf16)
+    hipLaunchKernelGGL(read_kv_bf16_kernel, dim3((unsigned)((all / 8 + 255) / 256)), dim3(256), 0, st, B, n, dm.Hkv, dm.D, Lmax,
+                       (const uint16_t*)kc, (const uint16_t*)vc, (uint16_t*)k, (uint16_t*)v);
+  else
+    hipLaunchKernelGGL(read_kv_f32_kernel, dim3((unsigned)((all + 255) / 256)), dim3(256), 0, st, B, n, dm.Hkv, dm.D, Lmax,
+                       (const float*)kc, (const float*)vc, (float*)k, (float*)v);
+}
+
 }  // namespace ssd

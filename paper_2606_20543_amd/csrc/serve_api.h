@@ -127,6 +127,29 @@ ssd_status attn_sizes(const ssd_kvq_cache* c, const ssd_kvq_attn_params* p, KvqA
   return SSD_OK;
 }
 
+// settings and arrays of a sampling call of R rows (logits: checked where they are the caller's)
+ssd_status sample_args(const ssd_sample_params& p, int R, const float* u, int32_t* tokens, float* probs, void* stream, SampleArgs& a,
+                       const float* logits = nullptr) {
+  if (!p.temperatures && (!std::isfinite(p.temperature) || p.temperature < 0.0))
+    return fail(SSD_E_INVAL, "temperature must be a finite number >= 0");
+  if ((!p.top_ps && std::isnan(p.top_p)) || (!p.min_ps && std::isnan(p.min_p)))
+    return fail(SSD_E_INVAL, "top_p and min_p must be numbers");
+  const size_t n = R;
+  ArrayCheck ck(stream);
+  if (logits) ck.need("logits", logits, span(n, p.ld, p.vocab, 4), 4);
+  ck.need("u", u, n * 4, 4);
+  ck.need("tokens", tokens, n * 4, 4);
+  if (probs) ck.need("probs", probs, n * 4, 4);
+  if (p.temperatures) ck.need("temperatures", p.temperatures, n * 4, 4);
+  if (p.top_ks) ck.need("top_ks", p.top_ks, n * 4, 4);
+  if (p.top_ps) ck.need("top_ps", p.top_ps, n * 4, 4);
+  if (p.min_ps) ck.need("min_ps", p.min_ps, n * 4, 4);
+  if (ck.bad) return ck.status();
+  a = SampleArgs{R, p.vocab, p.top_k, 0, (size_t)p.ld, p.temperature, p.top_p, p.min_p, p.temperatures, p.top_ps, p.min_ps, p.top_ks,
+                 logits, u, tokens, probs};
+  return SSD_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -286,25 +309,83 @@ ssd_status ssd_sample_logits(const ssd_sample_params* p, int32_t R, const float*
   if (R < 1) return fail(SSD_E_INVAL, "R = %d must be positive", R);
   if (p->vocab < 1 || p->vocab > (1 << 18)) return fail(SSD_E_INVAL, "vocab = %d outside [1, 2^18]", p->vocab);
   if (p->ld < p->vocab) return fail(SSD_E_INVAL, "ld must be at least vocab");
-  if (!p->temperatures && (!std::isfinite(p->temperature) || p->temperature < 0.0))
-    return fail(SSD_E_INVAL, "temperature must be a finite number >= 0");
-  if ((!p->top_ps && std::isnan(p->top_p)) || (!p->min_ps && std::isnan(p->min_p)))
-    return fail(SSD_E_INVAL, "top_p and min_p must be numbers");
-  const size_t n = R;
-  ArrayCheck ck(stream);
-  ck.need("logits", logits, span(n, p->ld, p->vocab, 4), 4);
-  ck.need("u", u, n * 4, 4);
-  ck.need("tokens", tokens, n * 4, 4);
-  if (probs) ck.need("probs", probs, n * 4, 4);
-  if (p->temperatures) ck.need("temperatures", p->temperatures, n * 4, 4);
-  if (p->top_ks) ck.need("top_ks", p->top_ks, n * 4, 4);
-  if (p->top_ps) ck.need("top_ps", p->top_ps, n * 4, 4);
-  if (p->min_ps) ck.need("min_ps", p->min_ps, n * 4, 4);
-  if (ck.bad) return ck.status();
-  sample_logits(SampleArgs{R, p->vocab, p->top_k, (size_t)p->ld, p->temperature, p->top_p, p->min_p, p->temperatures,
-                           p->top_ps, p->min_ps, p->top_ks, logits, u, tokens, probs},
-                (hipStream_t)stream);
+  SampleArgs a;
+  const ssd_status cs = sample_args(*p, R, u, tokens, probs, stream, a, logits);
+  if (cs != SSD_OK) return cs;
+  sample_logits(a, (hipStream_t)stream);
   return launched("ssd_sample_logits");
+}
+
+ssd_status ssd_session_sample(ssd_session* s, const ssd_sample_params* p, const float* u, int32_t* tokens, float* probs) {
+  g_err.clear();
+  if (!s || !p || !u || !tokens) return fail(SSD_E_INVAL, "NULL argument");
+  if (s->poisoned) return fail(SSD_E_STATE, "session is poisoned");
+  if (s->dm.Vimg > (1 << 18)) return fail(SSD_E_INVAL, "sampling takes up to 2^18 codes");
+  SampleArgs a;
+  const ssd_status cs = sample_args(*p, s->Bi, u, tokens, probs, s->stream, a);
+  if (cs != SSD_OK) return cs;
+  a.V = s->dm.Vimg;
+  a.ld = (size_t)s->dm.Vimg;
+  a.add = s->dm.img_lo;
+  a.logits = s->carry;
+  if (s->cfg) {
+    cfg_mix(s->Bi, 0, s->dm.Vimg, s->cfg_w, nullptr, s->carry, nullptr, s->mcarry, s->stream);
+    a.logits = s->mcarry;
+  }
+  sample_logits(a, s->stream);
+  return launched("ssd_session_sample");
+}
+
+ssd_status ssd_session_set_axes(ssd_session* s, int32_t n_axes, const int32_t* section, const int32_t* positions) {
+  g_err.clear();
+  if (!s || !section || !positions) return fail(SSD_E_INVAL, "NULL argument");
+  if (s->poisoned) return fail(SSD_E_STATE, "session is poisoned");
+  if (n_axes < 1 || n_axes > SSD_ROPE_AXES) return fail(SSD_E_INVAL, "n_axes = %d outside [1, %d]", n_axes, SSD_ROPE_AXES);
+  RopeTableArgs a{};
+  int64_t half = 0;
+  for (int i = 0; i < n_axes; ++i) {
+    if (section[i] < 0) return fail(SSD_E_INVAL, "negative section");
+    half += section[i];
+    a.section[i] = section[i];
+  }
+  if (half != s->dm.D / 2) return fail(SSD_E_INVAL, "sections sum to %lld pairs, a head has %d", (long long)half, s->dm.D / 2);
+  a.n = s->max_ctx - s->P;  // (at least one)
+  for (int b = 0; b < s->B; ++b)
+    if (s->f[b] != s->P) return fail(SSD_E_STATE, "positions behind the prompt are already committed");
+  try {
+    if (!s->axes) s->axes = s->mem.get<int>((size_t)SSD_ROPE_AXES * a.n);
+  } catch (HipError& e) {
+    return fail(SSD_E_OOM, "%s: %s", e.what, hipGetErrorString(e.e));
+  }
+  if (hipMemcpyAsync(s->axes, positions, (size_t)n_axes * a.n * 4, hipMemcpyDefault, s->stream) != hipSuccess) {
+    (void)hipGetLastError();
+    return fail(SSD_E_INVAL, "the positions could not be read");
+  }
+  a.pos = s->axes;
+  a.half = s->dm.D / 2;
+  a.theta = (double)s->dm.theta;
+  a.tab = s->rope + (size_t)s->P * a.half;
+  rope_axes_table(a, s->stream);
+  const ssd_status ls = launched("ssd_session_set_axes");
+  if (ls != SSD_OK) s->poisoned = true;
+  return ls;
+}
+
+ssd_status ssd_session_read_kv(ssd_session* s, int32_t layer, int32_t n, void* k_out, void* v_out) {
+  g_err.clear();
+  if (!s || !k_out || !v_out) return fail(SSD_E_INVAL, "NULL argument");
+  if (s->poisoned) return fail(SSD_E_STATE, "session is poisoned");
+  if (layer < 0 || layer >= s->dm.L) return fail(SSD_E_INVAL, "layer = %d of %d", layer, s->dm.L);
+  for (int b = 0; b < s->B; ++b)
+    if (n < 1 || n > s->f[b]) return fail(SSD_E_INVAL, "n = %d outside [1, frontier = %d]", n, s->f[b]);
+  const size_t es = esize(s->dm), bytes = (size_t)s->B * n * s->dm.Hkv * s->dm.D * es;
+  ArrayCheck ck(s->stream);
+  ck.need("k_out", k_out, bytes, 16);
+  ck.need("v_out", v_out, bytes, 16);
+  if (ck.bad) return ck.status();
+  const size_t at = (size_t)layer * s->kv_layer_elems * es;
+  read_kv(s->dm, s->B, n, s->Lmax, (const char*)s->kc + at, (const char*)s->vc + at, k_out, v_out, s->stream);
+  return launched("ssd_session_read_kv");
 }
 
 }  // extern "C"

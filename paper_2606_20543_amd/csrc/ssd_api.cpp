@@ -464,6 +464,7 @@ struct ssd_session {
   void* vc;
   size_t kv_layer_elems;
   float2* rope;
+  int* axes = nullptr;  // positions of ssd_session_set_axes
   float* gpart;
   int ssq_parts_cap;
   size_t gpart_cap;

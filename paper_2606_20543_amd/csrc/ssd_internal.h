@@ -455,7 +455,7 @@ struct RopeArgs {
 };
 void rope_axes(const RopeArgs& a, hipStream_t st);
 struct SampleArgs {
-  int R, V, top_k;
+  int R, V, top_k, add;  // add: id of the first code
   size_t ld;
   double temperature, top_p, min_p;
   const float *temperatures, *top_ps, *min_ps;  // [R], or nullptr: the number for all rows
@@ -465,6 +465,17 @@ struct SampleArgs {
   float* probs;  // or nullptr
 };
 void sample_logits(const SampleArgs& a, hipStream_t st);
+// rotary factors of n positions with several axes, as rope_table lays them out
+struct RopeTableArgs {
+  float2* tab;
+  int n, half;
+  int section[SSD_ROPE_AXES];
+  double theta;
+  const int* pos;  // [axes][n]
+};
+void rope_axes_table(const RopeTableArgs& a, hipStream_t st);
+// a layer's cached keys and values of positions [0, n) as rows [B][n][Hkv][D]
+void read_kv(const Dims& dm, int B, int n, int Lmax, const void* kc, const void* vc, void* k, void* v, hipStream_t st);
 struct KvqAppendArgs {
   uint8_t *kc, *vc, *ke, *ve;
   int n_blocks, T, Hkv, D, n_rows, bf16;
