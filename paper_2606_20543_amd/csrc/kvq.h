@@ -49,12 +49,18 @@ __device__ __forceinline__ void kvq_value4(uint32_t codes, float (&v)[4]) {
 
 // ---------------- writing ----------------
 // Row r of the new keys and values goes to slot slots[r] (block * T + offset);
-// negative and too large slots are skipped.  A wave owns one run: the rows of
-// one block, consecutive rows with consecutive slots.  It starts at a row
-// whose predecessor is not the slot before it, or at a block's first slot; the
-// other rows' waves end at once.  The wave finds the run's largest magnitude,
-// sets the scale, rewrites the block's older codes where the scale grew, and
-// stores the run (which it reads a second time, from the caches).
+// negative and too large slots are skipped.  A run is the rows of one block:
+// consecutive rows with consecutive slots.  It starts at a row whose
+// predecessor is not the slot before it, or at a block's first slot.  A run's
+// largest magnitude gives the scale; the block's older codes are rewritten where
+// the scale grew, then the run is stored.
+//
+// Nothing is computed to speak of: the bytes bound it (8 heads of 128, 16 prompts of 2048
+// rows after one: 134 MB, 26 us at the rate of a large copy; 41 us a call, 36 of them the
+// kernel), and, for single tokens, the launch (7.4 us a call).  Where a window of rows starts one or
+// two runs, a workgroup takes them together and holds the elements between the maximum and the
+// codes, so the rows are read once; where it starts more (short runs), a wave takes each and
+// reads it a second time, from the caches (every run by a wave of its own: 47 us for the prompts).
 template <typename E>
 __device__ __forceinline__ float kvq_ld(const E* p);
 template <>
@@ -80,25 +86,33 @@ struct alignas(ALIGNED ? sizeof(E) * N : sizeof(E)) KvqVec {
   E v[N];
 };
 
+// a run's row r, in elements
+template <bool NEAR>
+__device__ __forceinline__ size_t kvq_row(int r, size_t ld) {
+  return NEAR ? (uint32_t)r * (uint32_t)ld : (size_t)r * ld;
+}
+__device__ __forceinline__ float kvq_max64(float m) {
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  return m;
+}
 // largest finite magnitude of n rows of D elements, in every lane: 16 bytes a lane and load where
 // the rows allow it (VEC), else two elements
 template <typename E, bool VEC>
 __device__ __forceinline__ float kvq_amax(const E* src, size_t ld, int n, int D, int lane) {
-  constexpr int N = VEC ? 16 / (int)sizeof(E) : 2, U = 8;  // U loads in flight (rows past the last: that one again)
+  constexpr int N = VEC ? 16 / (int)sizeof(E) : 2, U = 4;  // U loads in flight (rows past the last: that one again)
   typedef KvqVec<E, N, VEC> V;
   const int per = D / N, step = 64 / per, c = (lane % per) * N;
   float m = 0.f;
   for (int r = lane / per; r < n; r += U * step) {
     V x[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) x[u] = *(const V*)(src + (size_t)min(r + u * step, n - 1) * ld + c);
+    for (int u = 0; u < U; ++u) x[u] = *(const V*)(src + kvq_row<VEC>(min(r + u * step, n - 1), ld) + c);
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int e = 0; e < N; ++e) m = fmaxf(m, kvq_mag(kvq_ld(&x[u].v[e])));
   }
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  return m;
+  return kvq_max64(m);
 }
 
 // codes times f (a power of two), rounded again, where keep has ones
@@ -112,13 +126,13 @@ __device__ __forceinline__ uint32_t kvq_low_bytes(int n) { return n >= 4 ? ~0u :
 // rows [0, n) of src to tokens off .. of a block's keys [T][D]
 template <typename E, bool VEC>
 __device__ __forceinline__ void kvq_put_keys(const E* src, size_t ld, int n, int D, int off, float inv, uint8_t* blk, int lane) {
-  constexpr int N = VEC ? 16 / (int)sizeof(E) : 2, U = 8;
+  constexpr int N = VEC ? 16 / (int)sizeof(E) : 2, U = 4;
   typedef KvqVec<E, N, VEC> V;
   const int per = D / N, step = 64 / per, c = (lane % per) * N;
   for (int r = lane / per; r < n; r += U * step) {
     V x[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) x[u] = *(const V*)(src + (size_t)min(r + u * step, n - 1) * ld + c);
+    for (int u = 0; u < U; ++u) x[u] = *(const V*)(src + kvq_row<VEC>(min(r + u * step, n - 1), ld) + c);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (r + u * step >= n) break;
@@ -136,6 +150,19 @@ __device__ __forceinline__ void kvq_put_keys(const E* src, size_t ld, int n, int
   }
 }
 
+// tokens t0 .. t0 + 15 of a dim's row, those in [off, end)
+__device__ __forceinline__ void kvq_put16(uint8_t* row, int t0, int off, int end, const float (&y)[16]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = kvq_code4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
+  if (t0 >= off && t0 + 16 <= end) {
+    *(uint4*)(row + t0) = make_uint4(w[0], w[1], w[2], w[3]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+      if (t0 + j >= off && t0 + j < end) row[t0 + j] = (uint8_t)(w[j / 4] >> (8 * (j % 4)));
+  }
+}
 // the same for values [D][T]: a lane owns two neighbouring dims and takes 16 tokens at a time, which
 // are 16 bytes of a dim's row where the run covers them all
 template <typename E, bool VEC>
@@ -146,106 +173,203 @@ __device__ __forceinline__ void kvq_put_values(const E* src, size_t ld, int n, i
   for (int t0 = (off & ~15) + 16 * (lane / per); t0 < off + n; t0 += 16 * groups) {
     V x[16];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) x[j] = *(const V*)(src + (size_t)min(max(t0 + j - off, 0), n - 1) * ld + d);
+    for (int j = 0; j < 16; ++j) x[j] = *(const V*)(src + kvq_row<VEC>(min(max(t0 + j - off, 0), n - 1), ld) + d);
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      uint8_t* p = blk + (size_t)(d + e) * T + t0;
-      uint32_t w[4];
+      float y[16];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        w[i] = kvq_code4(kvq_fit(kvq_ld(&x[4 * i].v[e]), inv), kvq_fit(kvq_ld(&x[4 * i + 1].v[e]), inv),
-                         kvq_fit(kvq_ld(&x[4 * i + 2].v[e]), inv), kvq_fit(kvq_ld(&x[4 * i + 3].v[e]), inv));
-      if (t0 >= off && t0 + 16 <= off + n) {
-        *(uint4*)p = make_uint4(w[0], w[1], w[2], w[3]);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-          if (t0 + j >= off && t0 + j < off + n) p[j] = (uint8_t)(w[j / 4] >> (8 * (j % 4)));
-      }
+      for (int j = 0; j < 16; ++j) y[j] = kvq_fit(kvq_ld(&x[j].v[e]), inv);
+      kvq_put16(blk + (size_t)(d + e) * T, t0, off, off + n, y);
     }
   }
 }
 
+// a run, for one head of the keys (which = 0) or the values
 template <typename E>
-__device__ __forceinline__ void kvq_append_run(const KvqAppendArgs& a, int which, int h, int row, int slot, int lane) {
-  const int T = a.T, D = a.D, off = slot & (T - 1), page = slot / T;
-  // length of the run
-  int n = 0;
-  while (true) {
-    const int r = row + n + lane;
-    const bool in = r < a.n_rows && off + n + lane < T && a.slots[min(r, a.n_rows - 1)] == slot + n + lane;
-    const uint64_t m = ~__ballot(in);
-    if (m) {
-      n += __builtin_ctzll(m);
-      break;
-    }
-    n += 64;
+struct KvqRun {
+  int n, off, page;  // rows; the first one's token in its block
+  const E* src;
+  size_t ld;
+  uint8_t *blk, *ep;
+  __device__ __forceinline__ KvqRun(const KvqAppendArgs& a, int which, int h, int row, int slot, int rows) {
+    const int T = a.T;
+    n = rows, off = slot & (T - 1), page = slot / T;
+    ld = which ? a.ld_v : a.ld_k;
+    src = (const E*)(which ? a.v : a.k) + (size_t)row * ld + (size_t)h * a.D;
+    blk = (which ? a.vc : a.kc) + ((size_t)page * a.Hkv + h) * ((size_t)T * a.D);
+    ep = (which ? a.ve : a.ke) + (size_t)page * a.Hkv + h;
   }
-  const size_t ld = which ? a.ld_v : a.ld_k;
-  const E* src = (const E*)(which ? a.v : a.k) + (size_t)row * ld + (size_t)h * D;
-  const bool vec = which ? a.vec_v : a.vec_k;  // 16-byte loads
-  uint8_t* blk = (which ? a.vc : a.kc) + ((size_t)page * a.Hkv + h) * ((size_t)T * D);
-  uint8_t* ep = (which ? a.ve : a.ke) + (size_t)page * a.Hkv + h;
-  const int old = off > 0 ? *ep : 0;
-  const float amax = vec ? kvq_amax<E, true>(src, ld, n, D, lane) : kvq_amax<E, false>(src, ld, n, D, lane);
-  const int s = max(kvq_exponent(amax), old);
-  if (off > 0 && s > old) {
+  // the codes before the run, by NT threads, where the exponent grew from old to s
+  template <int NT>
+  __device__ __forceinline__ void rescale(int which, int T, int D, int old, int s, int t) const {
+    if (off == 0 || s <= old) return;
     // 2^(old - s): a factor below every code's smallest part leaves zero
     const float f = old - s < -126 ? 0.f : kvq_pow2(old - s);
     if (which) {
       const int words = (off + 3) / 4;
-      for (int i = lane; i < words * D; i += 64) {
+      for (int i = t; i < words * D; i += NT) {
         uint32_t* p = (uint32_t*)(blk + (size_t)(i / words) * T) + i % words;
         *p = kvq_again(*p, f, kvq_low_bytes(off - 4 * (i % words)));
       }
     } else {
-      for (int i = lane; i < off * D / 4; i += 64) {
+      for (int i = t; i < off * D / 4; i += NT) {
         uint32_t* p = (uint32_t*)blk + i;
         *p = kvq_again(*p, f, ~0u);
       }
     }
   }
-  if (lane == 0) *ep = (uint8_t)s;
+};
+// The exponent for a workgroup's elements (m: a thread's largest), set; returns the factor of the codes.
+template <typename E>
+__device__ __forceinline__ float kvq_shared_scale(const KvqRun<E>& run, int which, int T, int D, float m, uint32_t* red) {
+  m = kvq_max64(m);
+  const int wave = threadIdx.x >> 6;
+  if ((threadIdx.x & 63) == 0) {
+    red[wave] = __float_as_uint(m);
+    if (wave == 0) red[4] = run.off > 0 ? *run.ep : 0;
+  }
+  __syncthreads();
+  const uint32_t top = max(max(red[0], red[1]), max(red[2], red[3]));  // of magnitudes: ordered like their bits
+  const int old = (int)red[4], s = max(kvq_exponent(__uint_as_float(top)), old);
+  run.template rescale<256>(which, T, D, old, s, threadIdx.x);
+  if (threadIdx.x == 0) *run.ep = (uint8_t)s;
+  return kvq_pow2(127 - s);
+}
+
+// a run by one wave
+template <typename E>
+__device__ __forceinline__ void kvq_append_run(const KvqAppendArgs& a, int which, const KvqRun<E>& run, int lane) {
+  const int T = a.T, D = a.D;
+  const int n = run.n, off = run.off, old = off > 0 ? *run.ep : 0;
+  const bool vec = which ? a.vec_v : a.vec_k;  // 16-byte loads
+  const float amax = vec ? kvq_amax<E, true>(run.src, run.ld, n, D, lane) : kvq_amax<E, false>(run.src, run.ld, n, D, lane);
+  const int s = max(kvq_exponent(amax), old);
+  run.template rescale<64>(which, T, D, old, s, lane);
+  if (lane == 0) *run.ep = (uint8_t)s;
   const float inv = kvq_pow2(127 - s);
   if (which) {
-    if (vec) kvq_put_values<E, true>(src, ld, n, D, T, off, inv, blk, lane);
-    else kvq_put_values<E, false>(src, ld, n, D, T, off, inv, blk, lane);
+    if (vec) kvq_put_values<E, true>(run.src, run.ld, n, D, T, off, inv, run.blk, lane);
+    else kvq_put_values<E, false>(run.src, run.ld, n, D, T, off, inv, run.blk, lane);
   } else {
-    if (vec) kvq_put_keys<E, true>(src, ld, n, D, off, inv, blk, lane);
-    else kvq_put_keys<E, false>(src, ld, n, D, off, inv, blk, lane);
+    if (vec) kvq_put_keys<E, true>(run.src, run.ld, n, D, off, inv, run.blk, lane);
+    else kvq_put_keys<E, false>(run.src, run.ld, n, D, off, inv, run.blk, lane);
   }
 }
 
-template <typename E>
+// A run by the workgroup's four waves, rows at 16-byte boundaries: a thread holds its elements
+// between the maximum and the codes, so that the rows are read once.  red: five words.
+template <typename E, int U>
+__device__ __forceinline__ void kvq_keys_shared(const KvqRun<E>& run, int T, int D, uint32_t* red) {
+  constexpr int N = 16 / (int)sizeof(E);
+  typedef KvqVec<E, N, true> V;
+  const int t = threadIdx.x, per = D / N, step = 256 / per, c = (t % per) * N, r0 = t / per;
+  V x[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) x[u] = *(const V*)(run.src + kvq_row<true>(min(r0 + u * step, run.n - 1), run.ld) + c);
+  float m = 0.f;
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int e = 0; e < N; ++e) m = fmaxf(m, kvq_mag(kvq_ld(&x[u].v[e])));
+  const float inv = kvq_shared_scale(run, 0, T, D, m, red);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int r = r0 + u * step;
+    if (r < run.n) {
+      KvqVec<uint32_t, N / 4, true> w;
+#pragma unroll
+      for (int e = 0; e < N / 4; ++e)
+        w.v[e] = kvq_code4(kvq_fit(kvq_ld(&x[u].v[4 * e]), inv), kvq_fit(kvq_ld(&x[u].v[4 * e + 1]), inv),
+                           kvq_fit(kvq_ld(&x[u].v[4 * e + 2]), inv), kvq_fit(kvq_ld(&x[u].v[4 * e + 3]), inv));
+      *(KvqVec<uint32_t, N / 4, true>*)(run.blk + (size_t)(run.off + r) * D + c) = w;
+    }
+  }
+}
+template <typename E, int G>
+__device__ __forceinline__ void kvq_values_shared(const KvqRun<E>& run, int T, int D, uint32_t* red) {
+  typedef KvqVec<E, 2, true> V;
+  const int t = threadIdx.x, per = D / 2, d = (t % per) * 2, off = run.off, end = off + run.n;
+  const int first = (off & ~15) + 16 * (t / per), stride = 16 * (256 / per);
+  V x[G][16];
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+      x[g][j] = *(const V*)(run.src + kvq_row<true>(min(max(first + g * stride + j - off, 0), run.n - 1), run.ld) + d);
+  float m = 0.f;
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int j = 0; j < 16; ++j) m = fmaxf(m, fmaxf(kvq_mag(kvq_ld(&x[g][j].v[0])), kvq_mag(kvq_ld(&x[g][j].v[1]))));
+  const float inv = kvq_shared_scale(run, 1, T, D, m, red);
+#pragma unroll
+  for (int g = 0; g < G; ++g)
+    if (first + g * stride < end)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float y[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) y[j] = kvq_fit(kvq_ld(&x[g][j].v[e]), inv);
+        kvq_put16(run.blk + (size_t)(d + e) * T, first + g * stride, off, end, y);
+      }
+}
+
+// A workgroup takes one side (keys or values of a head) of a window of rows: the runs that start there.
+// R: what a thread holds of a shared run covers 8192 R elements (a block has up to 128 x 128).
+template <typename E, int R>
 __global__ __launch_bounds__(256) void kvq_append_kernel(KvqAppendArgs a) {
-  const int lane = threadIdx.x & 63;
-  const long long task = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  __shared__ uint32_t red[2][5];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   // windows of rows fastest: the few that start a run in long prompts then fall on all XCDs alike
-  const int windows = (a.n_rows + a.window - 1) / a.window, side = (int)(task / windows), which = side & 1, h = side >> 1;
-  const long long first = task % windows * a.window;
-  if (h >= a.Hkv) return;
-  // the runs that start among this wave's rows
-  const int cap = a.n_blocks * a.T, r = (int)min(first + lane, (long long)a.n_rows - 1);
-  const int slot = a.slots[r], prev = r > 0 ? a.slots[r - 1] : -2;
-  const bool starts = lane < a.window && first + lane < a.n_rows && slot >= 0 && slot < cap &&
-                      ((slot & (a.T - 1)) == 0 || prev != slot - 1);
-  for (uint64_t m = __ballot(starts); m; m &= m - 1) {
-    const int l = __builtin_ctzll(m);
-    kvq_append_run<E>(a, which, h, (int)first + l, __builtin_amdgcn_readlane(slot, l), lane);
+  const int windows = (a.n_rows + a.window - 1) / a.window, side = (int)(blockIdx.x / windows), which = side & 1, h = side >> 1;
+  const int first = (int)(blockIdx.x % windows) * a.window;
+  const int cap = a.n_blocks * a.T, last = a.n_rows - 1;
+  // slots of the window's rows and of those that a run from it can reach (a block has at most 128),
+  // read together; stop: the rows that do not continue the run before them
+  int slot[3], prev[3];
+  uint64_t stop[3];
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    const int r = (int)min((long long)first + 64 * i + lane, (long long)last);
+    slot[i] = a.slots[r], prev[i] = a.slots[max(r - 1, 0)];
+  }
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    const long long r = (long long)first + 64 * i + lane;
+    stop[i] = __ballot(r > last || r == 0 || (slot[i] & (a.T - 1)) == 0 || prev[i] != slot[i] - 1);
+  }
+  uint64_t m = stop[0] & __ballot(lane < a.window && (long long)first + lane <= last && slot[0] >= 0 && slot[0] < cap);
+  const bool shared = (which ? a.vec_v : a.vec_k) && __builtin_popcountll(m) <= 2;
+  for (int i = 0; m; m &= m - 1, ++i) {
+    const int l = __builtin_ctzll(m), s0 = __builtin_amdgcn_readlane(slot[0], l);
+    if (!shared && (i & 3) != wave) continue;
+    // rows to the next one that starts anew
+    const uint64_t rest = l < 63 ? stop[0] >> (l + 1) : 0;
+    int n = 64 - l;
+    if (rest) n = 1 + __builtin_ctzll(rest);
+    else if (stop[1]) n += __builtin_ctzll(stop[1]);
+    else n += 64 + (stop[2] ? __builtin_ctzll(stop[2]) : 64);
+    const KvqRun<E> run(a, which, h, first + l, s0, n);
+    if (!shared) kvq_append_run<E>(a, which, run, lane);
+    else if (which) kvq_values_shared<E, R>(run, a.T, a.D, red[i & 1]);
+    else kvq_keys_shared<E, R * (sizeof(E) == 2 ? 4 : 8)>(run, a.T, a.D, red[i & 1]);
   }
 }
 
 void kvq_append(KvqAppendArgs a, hipStream_t st) {
   const int es = a.bf16 ? 2 : 4;
-  a.vec_k = (((uintptr_t)a.k | a.ld_k * es) & 15) == 0;
-  a.vec_v = (((uintptr_t)a.v | a.ld_v * es) & 15) == 0;
-  // rows that a wave looks at: one while that makes few enough waves (each may start a run: a step
-  // of single tokens), more for long prompts, where one in a block's rows does
-  a.window = std::max(1, std::min(16, a.n_rows / 1024));
-  const long long tasks = (long long)((a.n_rows + a.window - 1) / a.window) * a.Hkv * 2;
-  const dim3 grid((unsigned)((tasks + 3) / 4));
-  if (a.bf16) hipLaunchKernelGGL(kvq_append_kernel<uint16_t>, grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL(kvq_append_kernel<float>, grid, dim3(256), 0, st, a);
+  // 16-byte loads, and 32 bits for an offset within a run
+  a.vec_k = (((uintptr_t)a.k | a.ld_k * es) & 15) == 0 && a.ld_k < (1 << 22);
+  a.vec_v = (((uintptr_t)a.v | a.ld_v * es) & 15) == 0 && a.ld_v < (1 << 22);
+  // Rows that a workgroup looks at: four while that makes few enough workgroups (each row may start a run, a
+  // step of single tokens), up to 64 for long prompts, where one in a block's rows does.  64 single
+  // tokens: 7.4 us a call with windows of 4, 16 with 16, 55 with 64; 16 prompts of 2048 rows: 116, 54, 41.
+  a.window = std::max(4, std::min(64, a.n_rows / 1024 * 4));
+  const dim3 grid((unsigned)((a.n_rows + a.window - 1) / a.window) * a.Hkv * 2);
+  const bool two = a.T * a.D > 64 * 128;
+  auto kernel = a.bf16 ? two ? kvq_append_kernel<uint16_t, 2> : kvq_append_kernel<uint16_t, 1>
+                       : two ? kvq_append_kernel<float, 2> : kvq_append_kernel<float, 1>;
+  hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a);
 }
 
 // ---------------- attention ----------------

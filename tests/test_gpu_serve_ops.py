@@ -218,6 +218,37 @@ def test_append(dev, dtype, block, kv, D, runs, extra, spread):
         assert_cache(arrs, plain)
 
 
+@pytest.mark.parametrize("dtype,block,D,rows,extra", [
+    ("bf16", 16, 64, 2100, 0), ("f32", 32, 128, 2500, 0), ("bf16", 64, 128, 17000, 0), ("bf16", 128, 128, 16500, 8),
+    ("f32", 128, 128, 17000, 4), ("f32", 128, 64, 5000, 0), ("bf16", 32, 64, 16400, 1)])
+def test_append_long(dev, dtype, block, D, rows, extra):
+    """Prompts of many blocks between single tokens and skipped rows: every length of the windows that look for runs."""
+    rng = np.random.default_rng(rows + block)
+    n_blocks = 2 * rows // block + 80
+    c, arrs, plain = cache_arrays(dev, rng, n_blocks, 1, block, D)
+    pages, slots = iter(rng.permutation(n_blocks).tolist()), []
+    while len(slots) < rows:
+        kind = rng.integers(4)
+        if kind == 0:
+            slots += [-1] * int(rng.integers(1, 70))
+        elif kind == 1:  # single tokens of several requests
+            slots += [next(pages) * block + int(rng.integers(block)) for _ in range(int(rng.integers(1, 9)))]
+        else:  # a prompt behind held tokens
+            off, left = int(rng.integers(block)), int(rng.integers(1, 20 * block))
+            while left > 0:
+                n = min(block - off, left)
+                p = next(pages) * block
+                slots += range(p + off, p + off + n)
+                off, left = 0, left - n
+    slots = np.array(slots[:rows], np.int32)
+    k, kval = rows_of(rng, rows, 1, D, dtype, D + extra, 3.0)
+    v, vval = rows_of(rng, rows, 1, D, dtype, D + extra, 3.0)
+    plain.append(slots, kval, vval)
+    ssd.ssd_kvq_append(c, ssd.ssd_kvq_append_params(code(dtype), rows, D + extra, D + extra), dev(slots).ptr,
+                       dev(k).ptr, dev(v).ptr)
+    assert_cache(arrs, plain)
+
+
 def test_append_special_values(dev):
     """Zeros, subnormal and huge magnitudes, infinities, NaN, values at 448 and half way between codes."""
     rng = np.random.default_rng(3)
