@@ -46,12 +46,65 @@ struct LsShared {
   int bi;
 };
 
-__device__ __forceinline__ unsigned long long ls_scan(unsigned long long v, int lane) {
-  for (int o = 1; o < 64; o <<= 1) {
-    const unsigned long long t = __shfl_up(v, o);
-    if (lane >= o) v += t;
-  }
-  return v;
+// Sums and extrema over lanes by moves between lanes of a row of 16 (no trip through shared memory);
+// every lane of the wave takes part.
+template <int CTRL, int ROWS = 15>
+__device__ __forceinline__ unsigned ls_move(unsigned v) {  // 0 where no lane gives one
+  return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 15, false);
+}
+template <int CTRL, int ROWS = 15>
+__device__ __forceinline__ float ls_move(float v) {
+  return __uint_as_float(ls_move<CTRL, ROWS>(__float_as_uint(v)));
+}
+template <int CTRL, int ROWS = 15>
+__device__ __forceinline__ unsigned long long ls_move(unsigned long long v) {
+  return (unsigned long long)ls_move<CTRL, ROWS>((unsigned)(v >> 32)) << 32 | ls_move<CTRL, ROWS>((unsigned)v);
+}
+constexpr int LS_ROR = 0x120, LS_SHR = 0x110, LS_BCAST15 = 0x142, LS_BCAST31 = 0x143;
+// op over each row's lanes, in all of them
+template <typename T, typename Op>
+__device__ __forceinline__ T ls_row(T v, Op op) {
+  v = op(v, ls_move<LS_ROR + 8>(v));
+  v = op(v, ls_move<LS_ROR + 4>(v));
+  v = op(v, ls_move<LS_ROR + 2>(v));
+  return op(v, ls_move<LS_ROR + 1>(v));
+}
+template <typename T, typename Op>
+__device__ __forceinline__ T ls_wave(T v, Op op) {
+  v = ls_row(v, op);
+  v = op(v, __shfl_xor(v, 16));
+  return op(v, __shfl_xor(v, 32));
+}
+// sums of the lanes up to each
+template <typename T>
+__device__ __forceinline__ T ls_scan(T v) {
+  v += ls_move<LS_SHR + 1>(v);
+  v += ls_move<LS_SHR + 2>(v);
+  v += ls_move<LS_SHR + 4>(v);
+  v += ls_move<LS_SHR + 8>(v);
+  v += ls_move<LS_BCAST15, 10>(v);         // into the odd rows
+  return v + ls_move<LS_BCAST31, 12>(v);   // into the upper half
+}
+struct LsAdd {
+  template <typename T>
+  __device__ __forceinline__ T operator()(T a, T b) const { return a + b; }
+};
+struct LsMax {
+  __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+struct LsMin {
+  __device__ __forceinline__ float operator()(float a, float b) const { return fminf(a, b); }
+};
+// over the waves' entries: the sum of those before the wave, of all
+static_assert(LS_W == 16, "a row of lanes");
+template <typename T>
+__device__ __forceinline__ T ls_before(const T* red, int lane, int wave) {
+  const T x = red[lane & 15];
+  return ls_row((lane & 15) < wave ? x : T(0), LsAdd{});
+}
+template <typename T>
+__device__ __forceinline__ T ls_all(const T* red, int lane) {
+  return ls_row(red[lane & 15], LsAdd{});
 }
 
 // a logit as it counts: NaN is never drawn, +inf is the largest finite number
@@ -102,12 +155,17 @@ struct LsRow {
           fn(beg + i * 256, x);
         }
     } else {
+      again(fn);
+    }
+  }
+  // the same, read from memory: for what few rows do (unrolled over held values it would take registers from all)
+  template <typename F>
+  __device__ __forceinline__ void again(F fn) const {
 #pragma unroll 2
-      for (int i = 0; i < groups; ++i) {
-        const float4 f = read(i);
-        const float x[4] = {f.x, f.y, f.z, f.w};
-        fn(beg + i * 256, x);
-      }
+    for (int i = 0; i < groups; ++i) {
+      const float4 f = read(i);
+      const float x[4] = {f.x, f.y, f.z, f.w};
+      fn(beg + i * 256, x);
     }
   }
 };
@@ -186,27 +244,15 @@ __device__ __forceinline__ LsCumul ls_histogram(const LsRow<NG>& row, const LsWe
   LsCumul q;
   q.ca = sh.cnt[2 * tid], q.cb = sh.cnt[2 * tid + 1];
   q.wa = sh.wgt[2 * tid], q.wb = sh.wgt[2 * tid + 1];
-  unsigned c = q.ca + q.cb;
-  for (int o = 1; o < 64; o <<= 1) {
-    const unsigned t = __shfl_up(c, o);
-    if (lane >= o) c += t;
-  }
-  q.c = c;
-  q.w = weigh ? ls_scan(q.wa + q.wb, lane) : 0;
+  q.c = ls_scan(q.ca + q.cb);
+  q.w = weigh ? ls_scan(q.wa + q.wb) : 0;
   if (lane == 63) {
     sh.cred[wave] = (unsigned)q.c;
     sh.wred[wave] = q.w;
   }
   __syncthreads();
-  q.c += c0;
-  q.w += w0;
-#pragma unroll  // (every wave's read: a loop to its own would wait for each)
-  for (int x = 0; x < LS_W - 1; ++x) {
-    const unsigned cx = sh.cred[x];
-    const unsigned long long wx = sh.wred[x];
-    q.c += x < wave ? cx : 0;
-    q.w += x < wave ? wx : 0;
-  }
+  q.c += c0 + ls_before(sh.cred, lane, wave);
+  q.w += w0 + ls_before(sh.wred, lane, wave);
   return q;
 }
 
@@ -257,10 +303,8 @@ __device__ __forceinline__ void ls_bound(const LsRow<NG>& row, const LsWeight& w
           }
         }
     });
-    for (int o = 32; o > 0; o >>= 1) {
-      mn = fminf(mn, __shfl_xor(mn, o));
-      mx = fmaxf(mx, __shfl_xor(mx, o));
-    }
+    mn = ls_wave(mn, LsMin{});
+    mx = ls_wave(mx, LsMax{});
     if (lane == 0) {
       sh.fmn[wave] = mn;
       sh.fmx[wave] = mx;
@@ -308,31 +352,23 @@ __device__ __forceinline__ void ls_bound(const LsRow<NG>& row, const LsWeight& w
       __syncthreads();
       return;
     }
-#pragma unroll
-    for (int x = 0; x < LS_W; ++x) {
-      mn = fminf(mn, sh.fmn[x]);
-      mx = fmaxf(mx, sh.fmx[x]);
-    }
+    mn = ls_row(sh.fmn[lane & 15], LsMin{});
+    mx = ls_row(sh.fmx[lane & 15], LsMax{});
     if (mn == mx) {
       // equal logits: so many of them, in code order
       const unsigned long long w1 = weigh ? LsWeight::fix(wt(mx)) : 0;
       unsigned take = goal.count - c0;
       if (goal.by_weight) take = w1 ? max((unsigned)fmin(ceil((goal.mass - (double)w0) / (double)w1), (double)n), 1u) : (unsigned)n;
       unsigned mine = 0;  // ties of this wave's segment, then those before it
-      row.each([&](int, const float(&x)[4]) {
+      row.again([&](int, const float(&x)[4]) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) mine += __popcll(__ballot(x[e] == mx));
       });
       __syncthreads();
       if (lane == 0) sh.cred[wave] = mine;
       __syncthreads();
-      unsigned at = 0;
-#pragma unroll
-      for (int x = 0; x < LS_W - 1; ++x) {
-        const unsigned cx = sh.cred[x];
-        at += x < wave ? cx : 0;
-      }
-      row.each([&](int v, const float(&x)[4]) {
+      unsigned at = ls_before(sh.cred, lane, wave);
+      row.again([&](int v, const float(&x)[4]) {
         unsigned k = at, all = 0;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -373,14 +409,13 @@ __global__ __launch_bounds__(LS_T) void sample_logits_kernel(SampleArgs a) {
   if (tid < LS_POW) sh.pow2[tid] = LS_ONE * exp2((double)tid / LS_POW);
   float mx = -INFINITY;
   row.each([&](int, const float(&x)[4]) { mx = fmaxf(mx, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]))); });
-  for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+  mx = ls_wave(mx, LsMax{});
   if (lane == 0) sh.fmx[wave] = mx;
   __syncthreads();
-#pragma unroll
-  for (int x = 0; x < LS_W; ++x) mx = fmaxf(mx, sh.fmx[x]);
+  mx = ls_row(sh.fmx[lane & 15], LsMax{});
   if (mx == -INFINITY || !(T > 0.0)) {  // nothing to draw, or the largest (its lowest code)
     int am = 0x7fffffff;
-    row.each([&](int v, const float(&x)[4]) {
+    row.again([&](int v, const float(&x)[4]) {
 #pragma unroll
       for (int e = 3; e >= 0; --e)
         if (x[e] == mx) am = min(am, v + e);
@@ -412,10 +447,7 @@ __global__ __launch_bounds__(LS_T) void sample_logits_kernel(SampleArgs a) {
       bi = sh.bi;
       mass = (double)sh.w0;
     } else {
-      unsigned long long all = 0;
-#pragma unroll
-      for (int x = 0; x < LS_W; ++x) all += sh.wred[x];
-      mass = (double)all;
+      mass = (double)ls_all(sh.wred, lane);
     }
     if (by_p) {  // (with a top-k the prefix ends inside that of the top-k)
       ls_bound(row, wt, bins, q, LsGoal{true, 0u, fmax(top_p * mass, 1.0)}, true, sh);
@@ -459,17 +491,11 @@ __global__ __launch_bounds__(LS_T) void sample_logits_kernel(SampleArgs a) {
       if constexpr (NG > 0) gs[i++] = t;
     });
   }
-  const unsigned long long inc = ls_scan((unsigned long long)s, lane);
+  const unsigned long long inc = ls_scan((unsigned long long)s);
   if (lane == 63) sh.wred[wave] = inc;
   if (tid == 0) sh.bi = 0x7fffffff;
   __syncthreads();
-  unsigned long long total = 0, base = 0;
-#pragma unroll
-  for (int x = 0; x < LS_W; ++x) {
-    const unsigned long long wx = sh.wred[x];
-    base += x < wave ? wx : 0;
-    total += wx;
-  }
+  const unsigned long long total = ls_all(sh.wred, lane), base = ls_before(sh.wred, lane, wave);
   const double target = (u > 0.0 ? u : 0.0) * (double)total;
   auto draw = [&](int v, float l) {
     a.tokens[r] = v + a.add;
@@ -480,23 +506,20 @@ __global__ __launch_bounds__(LS_T) void sample_logits_kernel(SampleArgs a) {
     unsigned long long run = base;
     int at = 0;
     bool found = false;
-    auto pass = [&](double t) {  // t: a group's sum
-      found |= (double)(run + (unsigned long long)t) > target;
-      run += found ? 0 : (unsigned long long)t;
+    auto pass = [&](double lanes) {  // a group's sum
+      const unsigned long long t = ls_wave((unsigned long long)lanes, LsAdd{});
+      found |= (double)(run + t) > target;
+      run += found ? 0 : t;
       at += found ? 0 : 1;
     };
     if constexpr (NG > 0) {
-      for (int o = 32; o > 0; o >>= 1)
-#pragma unroll
-        for (int g = 0; g < NG; ++g) gs[g] += __shfl_xor(gs[g], o);
 #pragma unroll
       for (int g = 0; g < NG; ++g) pass(gs[g]);
     } else {
       row.each([&](int v, const float(&x)[4]) {
         if (found) return;
-        double w[4], t = group_sum(v, x, w);
-        for (int o = 32; o > 0; o >>= 1) t += __shfl_xor(t, o);
-        pass(t);
+        double w[4];
+        pass(group_sum(v, x, w));
       });
     }
     const float4 f = row.read(at);
@@ -504,7 +527,7 @@ __global__ __launch_bounds__(LS_T) void sample_logits_kernel(SampleArgs a) {
     const int v = row.beg + at * 256;
     double w[4];
     const unsigned long long t = (unsigned long long)group_sum(v, x, w);
-    unsigned long long c = run + (ls_scan(t, lane) - t);
+    unsigned long long c = run + (ls_scan(t) - t);
     if (!((double)c > target) && (double)(c + t) > target) {
       found = false;
 #pragma unroll
@@ -520,7 +543,7 @@ __global__ __launch_bounds__(LS_T) void sample_logits_kernel(SampleArgs a) {
   __syncthreads();
   if (sh.bi == 0x7fffffff) {  // u at or past one: the last code that has a weight
     int last = -1;
-    row.each([&](int v, const float(&x)[4]) {
+    row.again([&](int v, const float(&x)[4]) {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         if (kept(x[e], v + e) && weight(x[e]) > 0.0) last = max(last, v + e);
