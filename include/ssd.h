@@ -556,7 +556,8 @@ ssd_status ssd_kvq_append(const ssd_kvq_cache* cache, const ssd_kvq_append_param
  * Errors: SSD_E_INVAL for NULL arrays, a bad cache, n_seqs, n_rows, max_q, max_len or
  * table_width < 1, n_heads no multiple of n_kv_heads, a row length below n_heads *
  * head_dim, an unknown dtype, a non-finite scale, too small a workspace,
- * n_seqs * max_q * n_heads of 2^31 or more, a table of more than 2^30 positions.
+ * n_seqs * max_q * n_heads of 2^31 or more, n_seqs * n_kv_heads * ceil(max_q * n_heads
+ * / n_kv_heads / 16) of 2^24 or more, a table of more than 2^30 positions.
  */
 typedef struct {
   int32_t dtype, n_seqs, n_rows, n_heads, max_q, max_len, table_width;
@@ -589,7 +590,7 @@ ssd_status ssd_kvq_attention(const ssd_kvq_cache* cache, const ssd_kvq_attn_para
  * temperatures, top_ks, top_ps, min_ps: NULL, or device arrays [R] (fp32, top_ks int32)
  * in place of the number for all rows; there a temperature that is not > 0 takes
  * the largest, and NaN for top_p or min_p switches it off.
- * Errors: SSD_E_INVAL for NULL arrays, R < 1, vocab outside [1, 2^18], ld < vocab, and a
+ * Errors: SSD_E_INVAL for NULL arrays, R outside [1, 2^22), vocab outside [1, 2^18], ld < vocab, and a
  * temperature that is negative or not finite, or a NaN top_p or min_p, as numbers.
  */
 typedef struct {

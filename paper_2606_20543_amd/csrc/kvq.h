@@ -732,7 +732,9 @@ struct KvqGeom {
 // Waves split the keys: a workgroup of four owns 16 QT rows of one (request, KV head)
 // and one share of its keys; wave w takes every fourth step, a step's codes in
 // registers while the next step's are on their way, and the four meet in LDS.
-// For few rows, where the cache's bytes bound it.
+// For few rows, where the cache's bytes bound it: single tokens of 64 requests of up to 16384, 8 heads
+// of 128, 1296 MB in 240 us, 5.4 TB/s (a large copy reads and writes 5.1); a single request of 412
+// is latency (7.5 us a call).
 template <typename E, int D, int QT>
 __global__ __launch_bounds__(256) void kvq_attn_keys_kernel(KvqAttnArgs a) {
   constexpr int ROWS = 16 * QT, RS = D + 4;
@@ -838,7 +840,11 @@ __global__ __launch_bounds__(256) void kvq_attn_keys_kernel(KvqAttnArgs a) {
 // of them the keys and half the values, into operands in LDS (32 KB at D = 128, two
 // steps' worth), while the codes of the next two steps are on their way in
 // registers; every wave multiplies the whole step with its own two tiles of 16
-// rows.  bf16 calls with many rows, where the matrix cores and the exponentials bound it.
+// rows.  bf16 calls with many rows.  8 x 64 rows of 32 heads, contexts to 4352 (19.6 GFLOP): 46 us
+// a call, 38 of them this kernel.  A step takes a workgroup 1.4 us, of which the products are 0.85 at
+// the matrix cores' peak; the rest of the call is the first codes' way in, the parts of the
+// shares (28 MB out, and in again by the merge) and the longest context's shares.  Running the next
+// step's first product under the exponentials (interleaved one to four instructions) measured the same.
 template <int D>
 struct KvqFromLds {
   const uint16_t* st;  // operands of 64 x 16 bytes: keys (t, kd), then values (dt, half)
@@ -936,6 +942,8 @@ __global__ __launch_bounds__(64 * NW, 2) void kvq_attn_rows_kernel(KvqAttnArgs a
   Raw ra, rb2;
   Two pa = place(key(0)), pb = place(key(1));
   load(ra, key(0), pa);
+  // (of two waves on a SIMD the one goes first: they take turns at the matrix core and the exponentials,
+  // 49.7 us in place of 52.6 for 8 x 64 rows at contexts to 4352; one wave a SIMD has no other)
   if (NW == 8 && wave < NW / 2) __builtin_amdgcn_s_setprio(1);
   KvqRows<D, QT, 1> rows;
   rows.start();
@@ -1042,42 +1050,50 @@ __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttnArgs a) {
   kvq_store4((E*)a.o + (size_t)(ge.r0 + r / g) * a.ld_o + (size_t)(h * g + r % g) * D + d, o, L);
 }
 
-// How a call is split (host): rows of a workgroup, and shares of the keys.
+// How a call is split (host): the kernel, rows of a workgroup and shares of the keys with the least
+// cost by a model of the longest context.
 //
-// Rows of one (request, KV head): up to 64 (and all fp32 calls) take the kernel whose waves split the
-// keys, 16 or 32 rows a workgroup; more the one whose waves split the rows, 256 or 128 rows a
-// workgroup, whichever pads them less (8 x 64 rows of four heads a KV head, contexts to 4352:
-// 46 us against 284 with 32 rows a workgroup).
+// Waves that split the keys (16 or 32 rows a workgroup; all fp32 calls): a round is 256 keys, 1.4 us
+// (1.0 at D = 64, 1.65 for 32 rows at D = 128) while the workgroups draw less than the HBM gives; rounds
+// in turn beyond about 200 workgroups (256: what the card holds of the widest), for contexts
+// are ragged and not all have their longest.  Waves that split the rows (256 or 128 a workgroup): a
+// round is 64 keys, 1.75 us while the workgroups fit the card, and 2 us for the start.  A second share
+// adds the merge: its launch, and a part for each share.
 //
-// Shares: the least of a cost model of the longest context.  A round (256 keys of a workgroup whose
-// waves split them, 64 where they split the rows) takes 1.4 (1.0 at D = 64) or 1.75 us while the workgroups draw less than
-// the HBM gives, or fit the CUs; more rounds in turn beyond about 200 workgroups (contexts are ragged:
-// not all have their longest).  A second share adds the merge: its launch, and a part for each share.
-// One token at 16000 keys, 8B heads: 15.0 us with 32 shares, 87 with one; 64 requests of up to 8000: 126 with
-// one, 132 to 189 with 2 to 32.
+// Measured (us a call, 8B heads, contexts ragged up to the length; keys split, 128 and 256 rows
+// a workgroup): 8 requests of 1000, 64 tokens: 26, 33, 33; 8 of 4000, 33 tokens: 33, 43, 40; 8 of
+// 4288, 64 tokens: 54, 49, 46; 8 of 4000, 80 tokens: 54, 52, 58; 32 of 2000, 64 tokens: 119,
+// 75, 73; a prompt of 2048: 114, 69, 72.  Shares: one token at 16000 keys 15.0 with 32, 87 with
+// one; 64 tokens at up to 8000: 126 with one, 132 to 189 with 2 to 32.
 void kvq_attn_plan(KvqAttnArgs& a) {
   const int rows = a.max_q * (a.Hq / a.Hkv);
-  auto padded = [&](int n) { return (rows + n - 1) / n * n; };
-  a.by_rows = !a.bf16 || rows <= 64 ? 0 : padded(256) * 9LL <= padded(128) * 10LL ? 8 : 4;
   a.qt = rows > 16 && a.bf16 ? 2 : 1;
-  a.group_rows = a.by_rows ? 32 * a.by_rows : 16 * a.qt;
-  a.groups = (rows + a.group_rows - 1) / a.group_rows;
-  a.rows_pad = a.groups * a.group_rows;
-  const double base = (double)a.B * a.Hkv * a.groups;
-  const int round = a.by_rows ? KVQ_STEP : 4 * KVQ_STEP;
-  const long long rounds = (a.max_len + round - 1) / round;
   double best = 0.0;
-  a.nsplit = 1;
-  for (int n = 1; n <= 64 && n <= rounds; ++n) {
-    const long long each = (rounds + n - 1) / n;
-    const double us = each * (a.by_rows ? 1.75 * std::max(1.0, base * n / (a.by_rows == 8 ? 340 : 680))
-                                        : (a.D == 64 ? 1.0 : 1.4) * std::max(1.0, base * n / 200)) +
-                      (n > 1 ? 2.5 + 0.25 * n + base * n * a.group_rows * a.D * 1e-6 : 0.0);
-    if (n == 1 || us < best) {
-      best = us;
-      a.nsplit = n;
+  int round = 0;
+  for (int by_rows : {0, 8, 4}) {
+    if (by_rows && !a.bf16) break;
+    const int group_rows = by_rows ? 32 * by_rows : 16 * a.qt, groups = (rows + group_rows - 1) / group_rows;
+    const double base = (double)a.B * a.Hkv * groups;
+    const int keys = by_rows ? KVQ_STEP : 4 * KVQ_STEP;
+    const long long rounds = (a.max_len + keys - 1) / keys;
+    const bool wide = a.qt == 2 && a.D == 128;
+    const double one = by_rows ? 1.75 : a.D == 64 ? 1.0 : wide ? 1.65 : 1.4;
+    const double fit = by_rows ? 2720.0 / by_rows : wide ? 256.0 : 200.0;
+    for (int n = 1; n <= 64 && n <= rounds; ++n) {
+      const double us = (rounds + n - 1) / n * one * std::max(1.0, base * n / fit) +
+                        (n > 1 ? 2.5 + 0.25 * n + base * n * group_rows * a.D * 1e-6 : 0.0) + (by_rows ? 2.0 : 0.0);
+      if (round == 0 || us < best) {
+        best = us;
+        round = keys;
+        a.by_rows = by_rows;
+        a.group_rows = group_rows;
+        a.groups = groups;
+        a.nsplit = n;
+      }
     }
   }
+  const long long rounds = (a.max_len + round - 1) / round;
+  a.rows_pad = a.groups * a.group_rows;
   a.chunk = (int)((rounds + a.nsplit - 1) / a.nsplit) * round;
   a.nsplit = (a.max_len + a.chunk - 1) / a.chunk;
 }

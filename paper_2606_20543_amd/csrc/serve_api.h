@@ -104,6 +104,9 @@ ssd_status attn_sizes(const ssd_kvq_cache* c, const ssd_kvq_attn_params* p, KvqA
     return fail(SSD_E_INVAL, "n_heads = %d must be a multiple of n_kv_heads = %d", p->n_heads, c->n_kv_heads);
   if ((int64_t)p->n_seqs * p->max_q > INT32_MAX / p->n_heads)
     return fail(SSD_E_INVAL, "n_seqs * max_q * n_heads must stay below 2^31");
+  const int64_t rows = (int64_t)p->max_q * (p->n_heads / c->n_kv_heads);
+  if ((int64_t)p->n_seqs * c->n_kv_heads * ((rows + 15) / 16) >= 1 << 24)
+    return fail(SSD_E_INVAL, "n_seqs * n_kv_heads * (max_q * query heads a KV head / 16, rounded up) must stay below 2^24");
   if ((int64_t)p->table_width * c->block > (1 << 30))
     return fail(SSD_E_INVAL, "table_width * block must be at most 2^30 positions");
   const int64_t cols = (int64_t)p->n_heads * c->head_dim;
@@ -306,7 +309,7 @@ ssd_status ssd_sample_logits(const ssd_sample_params* p, int32_t R, const float*
                              float* probs, void* stream) {
   g_err.clear();
   if (!p || !logits || !u || !tokens) return fail(SSD_E_INVAL, "NULL argument");
-  if (R < 1) return fail(SSD_E_INVAL, "R = %d must be positive", R);
+  if (R < 1 || R >= 1 << 22) return fail(SSD_E_INVAL, "R = %d outside [1, 2^22)", R);
   if (p->vocab < 1 || p->vocab > (1 << 18)) return fail(SSD_E_INVAL, "vocab = %d outside [1, 2^18]", p->vocab);
   if (p->ld < p->vocab) return fail(SSD_E_INVAL, "ld must be at least vocab");
   SampleArgs a;

@@ -350,6 +350,55 @@ def test_attention(dev, dtype, heads, kv, D, block, reqs):
     assert_attend(got, want, tol)
 
 
+MANY = [  # heads, kv, D, block, table width, (len, rows) of every request, hidden entries, more
+    # (wide tables and many requests: sizes at which the waves of a workgroup split the rows, 256 and 128 of them)
+    (32, 8, 128, 64, 68, [(1500, 64), (903, 50), (0, 0), (64, 64), (3, 8), (705, 33), (129, 1), (1000, 40)], [], {}),
+    (32, 8, 128, 64, 68, [(1400, 64), (900, 63), (0, 2), (65, 64), (448, 60), (705, 33), (130, 17), (3, 8)],
+     [(0, 3, -1), (0, 22, 10 ** 6), (1, 0, -2 ** 31), (4, 6, -1)], dict(extra=3)),
+    (32, 8, 128, 32, 128, [(1500, 80), (700, 66), (81, 80), (5, 1), (333, 40), (0, 0), (900, 8), (64, 70)],
+     [(1, 2, -1)], dict(q_scale=60.0)),
+    (32, 8, 64, 16, 272, [(1300, 64), (200, 50), (64, 64), (63, 64), (705, 33), (129, 1), (900, 40), (2, 2)],
+     [(4, 0, -1), (4, 1, -1)], dict(extra=1, scale=-0.3)),
+    (32, 8, 64, 128, 34, [(1200, 80), (900, 66), (128, 80), (5, 6), (333, 40), (0, 0), (900, 8), (64, 70)], [],
+     dict(max_q=79)),
+    (16, 16, 128, 64, 256, [(2600, 130), (131, 130), (700, 20)], [(0, 40, -1)], dict(max_len=9000)),
+    (24, 8, 128, 128, 128, [(2000, 90), (91, 90), (1, 1)], [], dict(max_len=10 ** 9))]
+
+
+@pytest.mark.parametrize("heads,kv,D,block,width,reqs,hide,more", MANY)
+def test_attention_many_rows(dev, heads, kv, D, block, width, reqs, hide, more):
+    rng = np.random.default_rng(heads + D + block)
+    more = dict(dict(max_len=width * block), **more)
+    got, want, tol, (c, p, dq, dcu, dl, dt, do, work, table, lens, *_) = attend_case(
+        dev, rng, "bf16", heads, kv, D, block, reqs, width=width, hide=hide, **more)
+    if "max_q" in more:  # rows past it are not computed
+        at = 0
+        for _, n in reqs:
+            want[at + more["max_q"]:at + max(n, more["max_q"])] = np.nan
+            at += n
+    assert_attend(got, want, tol)
+    # in place, with anything in the codes that no row sees
+    k, v = dev.all[0].numpy().copy().reshape(c.n_blocks, kv, block, D), dev.all[1].numpy().copy().reshape(c.n_blocks, kv, D, block)
+    ke, ve = dev.all[2].numpy().copy().reshape(c.n_blocks, kv), dev.all[3].numpy().copy().reshape(c.n_blocks, kv)
+    used = {}
+    for b, L in enumerate(lens):
+        for j in range(min(width, -(-int(L) // block))):
+            used[int(table[b, j])] = min(block, int(L) - block * j)
+    for pg in range(c.n_blocks):
+        n = used.get(pg, 0)
+        k[pg, :, n:], v[pg, :, :, n:] = 0x7F, 0xFF
+        if n == 0:
+            ke[pg], ve[pg] = 255, 255
+    for a, x in zip(dev.all[:4], (k, v, ke, ve)):
+        upload(a, x)
+    before = values(dq, "bf16").reshape(-1, p.ld_q)
+    ssd.ssd_kvq_attention(c, p, dq.ptr, dcu.ptr, dl.ptr, dt.ptr, dq.ptr, work.ptr)
+    after = values(dq, "bf16").reshape(-1, p.ld_q)
+    none = np.isnan(want).all((1, 2))
+    assert (after[none] == before[none]).all() and (after[:, heads * D:] == before[:, heads * D:]).all()
+    assert np.array_equal(after[~none][:, :heads * D].reshape(-1, heads, D), got[~none])
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_attention_strides_and_wrong_hints(dev, dtype):
     """Rows with a gap, a max_len hint far too small and far too large."""

@@ -114,7 +114,7 @@ def test_attention_refusals(lib):
     cases += [(c, change(p, **kw), word) for kw, word in (
         (dict(dtype=-1), "dtype"), (dict(n_seqs=0), "positive"), (dict(n_rows=0), "positive"), (dict(max_q=0), "positive"),
         (dict(max_len=0), "positive"), (dict(table_width=0), "positive"), (dict(n_heads=5), "n_heads"), (dict(n_heads=0), "n_heads"),
-        (dict(n_seqs=2 ** 15, max_q=2 ** 14), "2^31"), (dict(table_width=2 ** 27), "2^30"), (dict(ld_q=255), "row lengths"), (dict(ld_out=255), "row lengths"),
+        (dict(n_seqs=2 ** 15, max_q=2 ** 14), "2^31"), (dict(n_seqs=2 ** 23, max_q=1), "2^24"), (dict(table_width=2 ** 27), "2^30"), (dict(ld_q=255), "row lengths"), (dict(ld_out=255), "row lengths"),
         (dict(scale=float("nan")), "scale"), (dict(scale=1e300), "scale"))]
     for cc, pp, word in cases:
         refused(ssd.ssd_kvq_attention, [cc, pp] + a, word)
@@ -134,6 +134,7 @@ def test_sample_refusals(lib):
                      (dict(top_p=nan), "top_p"), (dict(min_p=nan), "min_p")):
         refused(ssd.ssd_sample_logits, [change(p, **kw), 2] + a, word)
     refused(ssd.ssd_sample_logits, [p, 0] + a, "R = 0")
+    refused(ssd.ssd_sample_logits, [p, 2 ** 22] + a, "R = 4194304")
     for i in range(3):
         refused(ssd.ssd_sample_logits, [p, 2] + a[:i] + [None] + a[i + 1:], "NULL")
 
