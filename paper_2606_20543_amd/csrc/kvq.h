@@ -55,7 +55,7 @@ __device__ __forceinline__ void kvq_value4(uint32_t codes, float (&v)[4]) {
 // largest magnitude gives the scale; the block's older codes are rewritten where
 // the scale grew, then the run is stored.
 //
-// Nothing is computed to speak of: the bytes bound it (8 heads of 128, 16 prompts of 2048
+// Nothing is computed to speak of: the bytes bound it (8 heads of 128, 16 prompts of up to 2048
 // rows after one: 134 MB, 26 us at the rate of a large copy; 41 us a call, 36 of them the
 // kernel), and, for single tokens, the launch (7.4 us a call).  Where a window of rows starts one or
 // two runs, a workgroup takes them together and holds the elements between the maximum and the
@@ -358,12 +358,12 @@ __global__ __launch_bounds__(256) void kvq_append_kernel(KvqAppendArgs a) {
 
 void kvq_append(KvqAppendArgs a, hipStream_t st) {
   const int es = a.bf16 ? 2 : 4;
-  // 16-byte loads, and 32 bits for an offset within a run
+  // 16-byte loads, and 32 bits for an offset within a run (16 prompts of up to 2048 rows: 36 us, 59 by elements)
   a.vec_k = (((uintptr_t)a.k | a.ld_k * es) & 15) == 0 && a.ld_k < (1 << 22);
   a.vec_v = (((uintptr_t)a.v | a.ld_v * es) & 15) == 0 && a.ld_v < (1 << 22);
   // Rows that a workgroup looks at: four while that makes few enough workgroups (each row may start a run, a
   // step of single tokens), up to 64 for long prompts, where one in a block's rows does.  64 single
-  // tokens: 7.4 us a call with windows of 4, 16 with 16, 55 with 64; 16 prompts of 2048 rows: 116, 54, 41.
+  // tokens: 7.4 us a call with windows of 4, 16 with 16, 55 with 64; 16 prompts of up to 2048 rows: 116, 54, 41.
   a.window = std::max(4, std::min(64, a.n_rows / 1024 * 4));
   const dim3 grid((unsigned)((a.n_rows + a.window - 1) / a.window) * a.Hkv * 2);
   const bool two = a.T * a.D > 64 * 128;
@@ -1011,7 +1011,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kvq_attn_rows_kernel(KvqAttnArgs a
 }
 
 // Joins the splits of rows that have more than one: D / 4 lanes a row and query head,
-// four splits' loads in flight together.  Bound by the bytes of the partial sums.
+// four splits' loads in flight together.  Bound by the bytes of the partial sums (28 MB in 8 us).
 template <typename E, int D>
 __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttnArgs a) {
   constexpr int LANES = D / 4;
@@ -1128,7 +1128,8 @@ void kvq_attention(KvqAttnArgs a, hipStream_t st) {
   a.part_s = (float2*)(a.part_o + kvq_part_rows(a) * a.D);
   // a negative scale turns the queries' signs; scores of a zero one are all 0 (not 0 * -inf where a key is hidden)
   a.neg = a.scale < 0.f;
-  a.vec = (((uintptr_t)a.q | a.ld_q * (a.bf16 ? 2 : 4)) & 15) == 0;  // rows start on 16 bytes (heads then do)
+  // rows start on 16 bytes, heads then do (8 x 64 rows of 32 heads: 46 us, 51 by elements)
+  a.vec = (((uintptr_t)a.q | a.ld_q * (a.bf16 ? 2 : 4)) & 15) == 0;
   a.scale_log2 = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-37f);
   if (a.bf16) {
     if (a.D == 128) kvq_launch<uint16_t, 128>(a, st);
