@@ -471,7 +471,7 @@ typedef struct {
  *           pool on by `used` and returns the blocks of finished requests.
  * Calling it again with the same inputs gives the same outputs.
  * Errors: SSD_E_INVAL for NULL arrays (pool may be NULL if n_pool = 0, slots and
- * positions if n_rows = 0) and sizes: block as above, n_seqs >= 1,
+ * positions if n_rows = 0) and sizes: block as above, n_seqs in [1, 2^20],
  * table_width >= 1, n_pool and n_rows >= 0.
  */
 typedef struct {

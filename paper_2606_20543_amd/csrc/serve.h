@@ -13,7 +13,8 @@ namespace ssd {
 // requests lack come from the pool in request order, so the first of request b
 // is pool[sum of the lacks before b].  A workgroup owns SLOT_SEQS requests and
 // sums the lengths of all requests before them itself (a few loads a thread),
-// so one launch does it with no hand-off between workgroups.  Bound by its
+// so one launch does it with no hand-off between workgroups; several share the rows
+// of the same requests where there are many.  Bound by its
 // launch and three dependent round trips (lengths, table or pool entry, store): 64
 // requests of one new token 7.6 us a call (4.9 the kernel), 2048 of up to 64 7.8 (7.1).
 constexpr int SLOT_T = 256, SLOT_SEQS = 8;
@@ -30,32 +31,40 @@ __device__ __forceinline__ int slot_blocks(long long n, int T, int sh, int width
 }
 
 __global__ __launch_bounds__(SLOT_T) void slots_kernel(SlotArgs a) {
-  __shared__ long long red[2][SLOT_T / 64];
+  __shared__ long long red[3][SLOT_T / 64];
   __shared__ int s_held[SLOT_SEQS], s_have[SLOT_SEQS];
-  __shared__ long long s_start[SLOT_SEQS + 1], s_cu[SLOT_SEQS + 1];
+  __shared__ long long s_start[SLOT_SEQS + 1], s_cu[SLOT_SEQS + 1], s_all;
   const int tid = threadIdx.x, b0 = blockIdx.x * SLOT_SEQS, nb = min(SLOT_SEQS, a.B - b0);
   const int T = a.T, W = a.width, sh = __builtin_ctz(a.T);  // (T is a power of two)
-  // rows and lacking blocks of the requests before this workgroup's
-  long long rows = 0, lack = 0;
-  for (int b = tid; b < b0; b += SLOT_T) {
+  const bool head = blockIdx.y == 0;  // writes what is not a row's
+  // rows and lacking blocks of the requests before this workgroup's, rows of all
+  long long rows = 0, lack = 0, all = 0;
+  for (int b = tid; b < a.B; b += SLOT_T) {
     const long long h = max(a.held[b], 0), n = max(a.fresh[b], 0);
-    rows += n;
-    lack += slot_blocks(h + n, T, sh, W) - slot_blocks(h, T, sh, W);
+    all += n;
+    if (b < b0) {
+      rows += n;
+      lack += slot_blocks(h + n, T, sh, W) - slot_blocks(h, T, sh, W);
+    }
   }
   rows = wave_sum_ll(rows);
   lack = wave_sum_ll(lack);
+  all = wave_sum_ll(all);
   if ((tid & 63) == 0) {
     red[0][tid >> 6] = rows;
     red[1][tid >> 6] = lack;
+    red[2][tid >> 6] = all;
   }
   __syncthreads();
   if (tid == 0) {
-    long long r = 0, l = 0;
+    long long r = 0, l = 0, t = 0;
     for (int w = 0; w < SLOT_T / 64; ++w) {
       r += red[0][w];
       l += red[1][w];
+      t += red[2][w];
     }
-    if (b0 == 0) a.cu[0] = 0;
+    s_all = t;
+    if (head && b0 == 0) a.cu[0] = 0;
     for (int i = 0; i < nb; ++i) {
       const long long h = max(a.held[b0 + i], 0), n = max(a.fresh[b0 + i], 0);
       s_held[i] = (int)h;
@@ -64,44 +73,52 @@ __global__ __launch_bounds__(SLOT_T) void slots_kernel(SlotArgs a) {
       s_start[i] = l;
       r += n;
       l += slot_blocks(h + n, T, sh, W) - s_have[i];
-      a.cu[b0 + i + 1] = (int)(r < INT_MAX ? r : INT_MAX);
-      a.lens[b0 + i] = (int)(h + n < INT_MAX ? h + n : INT_MAX);
+      if (head) {
+        a.cu[b0 + i + 1] = (int)(r < INT_MAX ? r : INT_MAX);
+        a.lens[b0 + i] = (int)(h + n < INT_MAX ? h + n : INT_MAX);
+      }
     }
     s_cu[nb] = r;
     s_start[nb] = l;
-    if (b0 + nb == a.B) a.used[0] = (int)(l < INT_MAX ? l : INT_MAX);
+    if (head && b0 + nb == a.B) a.used[0] = (int)(l < INT_MAX ? l : INT_MAX);
   }
   __syncthreads();
   // table entries of the blocks taken here (an empty pool leaves -1)
   auto pooled = [&](long long i) { return i < a.n_pool ? a.pool[i] : -1; };
-  for (long long e = s_start[0] + tid; e < s_start[nb]; e += SLOT_T) {
+  for (long long e = s_start[0] + tid; head && e < s_start[nb]; e += SLOT_T) {
     int i = 0;
     while (s_start[i + 1] <= e) ++i;
     a.table[(size_t)(b0 + i) * W + s_have[i] + (e - s_start[i])] = pooled(e);
   }
-  // new rows, and behind the last request the padding
-  const long long last = b0 + nb == a.B ? a.n_rows : min(s_cu[nb], (long long)a.n_rows);
-  for (long long r = s_cu[0] + tid; r < last; r += SLOT_T) {
-    int slot = -1, pos = -1;
-    if (r < s_cu[nb]) {
-      int i = 0;
-      while (s_cu[i + 1] <= r) ++i;
-      const long long p = s_held[i] + (r - s_cu[i]);
-      const long long j = p >> sh;
-      pos = (int)(p < INT_MAX ? p : INT_MAX);
-      if (j < W) {
-        const int page = j >= s_have[i] ? pooled(s_start[i] + (j - s_have[i])) : a.table[(size_t)(b0 + i) * W + j];
-        const long long at = (long long)page * T + (p & (T - 1));
-        if (page >= 0 && at <= INT_MAX) slot = (int)at;
-      }
+  // new rows
+  const long long last = min(s_cu[nb], (long long)a.n_rows);
+  for (long long r = s_cu[0] + blockIdx.y * SLOT_T + tid; r < last; r += gridDim.y * SLOT_T) {
+    int i = 0, slot = -1;
+    while (s_cu[i + 1] <= r) ++i;
+    const long long p = s_held[i] + (r - s_cu[i]);
+    const long long j = p >> sh;
+    if (j < W) {
+      const int page = j >= s_have[i] ? pooled(s_start[i] + (j - s_have[i])) : a.table[(size_t)(b0 + i) * W + j];
+      const long long at = (long long)page * T + (p & (T - 1));
+      if (page >= 0 && at <= INT_MAX) slot = (int)at;
     }
     a.slots[r] = slot;
-    a.positions[r] = pos;
+    a.positions[r] = (int)(p < INT_MAX ? p : INT_MAX);
   }
+  // rows behind the last request's
+  const long long w = (long long)blockIdx.y * gridDim.x + blockIdx.x;
+  for (long long r = s_all + w * SLOT_T + tid; r < a.n_rows; r += (long long)gridDim.x * gridDim.y * SLOT_T)
+    a.slots[r] = a.positions[r] = -1;
 }
 
 void kvq_slots(const SlotArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL(slots_kernel, dim3((a.B + SLOT_SEQS - 1) / SLOT_SEQS), dim3(SLOT_T), 0, st, a);
+  // Workgroups for the same requests' rows: one for each 1024 of the rows that a group gets on average (a
+  // prompt of 65536: 88 us with one, 4.6 with 64), and with many rows up to four for a group that gets more (one
+  // such prompt among 2047 single tokens: 91 us with one, 31 with four, 26 with eight, which take
+  // 0.9 us longer where all groups get the same).
+  const int groups = (a.B + SLOT_SEQS - 1) / SLOT_SEQS;
+  const int parts = std::max({1, std::min(256, a.n_rows / 1024 / groups), std::min(4, a.n_rows / 16384)});
+  hipLaunchKernelGGL(slots_kernel, dim3(groups, parts), dim3(SLOT_T), 0, st, a);
 }
 
 // ---------------- rotary positions with several axes ----------------

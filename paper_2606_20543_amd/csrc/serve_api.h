@@ -165,6 +165,7 @@ ssd_status ssd_kvq_slots(const ssd_kvq_slot_params* p, const int32_t* held, cons
   if (!block_ok(p->block)) return fail(SSD_E_INVAL, "block = %d: 16, 32, 64 or 128 tokens", p->block);
   if (p->n_seqs < 1 || p->table_width < 1 || p->n_pool < 0 || p->n_rows < 0)
     return fail(SSD_E_INVAL, "n_seqs and table_width must be positive, n_pool and n_rows not negative");
+  if (p->n_seqs > 1 << 20) return fail(SSD_E_INVAL, "n_seqs = %d: up to 2^20 requests", p->n_seqs);
   if (!held || !fresh || !table || !lens || !cu || !used || (p->n_pool && !pool) || (p->n_rows && (!slots || !positions)))
     return fail(SSD_E_INVAL, "NULL argument");
   const size_t B = p->n_seqs, n = p->n_rows;
@@ -363,6 +364,10 @@ ssd_status ssd_session_set_axes(ssd_session* s, int32_t n_axes, const int32_t* s
   if (hipMemcpyAsync(s->axes, positions, (size_t)n_axes * a.n * 4, hipMemcpyDefault, s->stream) != hipSuccess) {
     (void)hipGetLastError();
     return fail(SSD_E_INVAL, "the positions could not be read");
+  }
+  if (!is_device_ptr(positions) && hipStreamSynchronize(s->stream) != hipSuccess) {  // the host's array may go at our return
+    (void)hipGetLastError();
+    return fail(SSD_E_DEVICE, "the positions' copy failed");
   }
   a.pos = s->axes;
   a.half = s->dm.D / 2;

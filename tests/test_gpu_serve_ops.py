@@ -79,7 +79,9 @@ def slot_case(rng, B, block, width, most_held, most_fresh, short=0, pad=0, cut=0
 SLOTS = [  # B, block, width, held, fresh, short of blocks, padded rows, rows cut
     (1, 16, 1, 0, 1, 0, 0, 0), (1, 16, 4, 15, 2, 0, 3, 0), (7, 16, 9, 100, 40, 0, 0, 0), (8, 32, 20, 500, 1, 0, 1, 0),
     (9, 64, 70, 4352, 0, 0, 4, 0), (64, 64, 69, 4352, 1, 0, 0, 0), (65, 128, 40, 3000, 700, 0, 17, 0),
-    (300, 16, 12, 150, 30, 0, 5, 0), (33, 16, 4, 90, 60, 0, 2, 0), (20, 16, 30, 200, 90, 11, 6, 0), (5, 32, 9, 64, 90, 0, 0, 40)]
+    (300, 16, 12, 150, 30, 0, 5, 0), (33, 16, 4, 90, 60, 0, 2, 0), (20, 16, 30, 200, 90, 11, 6, 0), (5, 32, 9, 64, 90, 0, 0, 40),
+    (1, 16, 5000, 9000, 60000, 0, 700, 0), (40, 64, 60, 800, 3000, 0, 20000, 0), (3, 128, 600, 0, 30000, 40, 0, 900),
+    (700, 32, 90, 2000, 40, 0, 33000, 0)]
 
 
 @pytest.mark.parametrize("B,block,width,held,fresh,short,pad,cut", SLOTS)

@@ -65,6 +65,7 @@ def test_slots_refusals(lib):
     a = [X] * 9
     for kw in (dict(block=0), dict(block=24), dict(block=256), dict(n_seqs=0), dict(table_width=0), dict(n_pool=-1), dict(n_rows=-1)):
         refused(ssd.ssd_kvq_slots, [change(p, **kw)] + a, "block =" if "block" in kw else "must be positive")
+    refused(ssd.ssd_kvq_slots, [change(p, n_seqs=2 ** 20 + 1)] + a, "2^20")
     for i in range(9):
         refused(ssd.ssd_kvq_slots, [p] + a[:i] + [None] + a[i + 1:], "NULL")
     assert lib.ssd_kvq_slots(None, *[None] * 10) == ssd.SSD_E_INVAL
