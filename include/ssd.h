@@ -496,7 +496,7 @@ ssd_status ssd_kvq_slots(const ssd_kvq_slot_params* params, const int32_t* held,
  * An output may be its input (same address and ld); otherwise they must not overlap.
  * positions int32 [n_axes][T], any value.  dtype SSD_F32 or SSD_BF16 (one rounding, of
  * the result).
- * Errors: SSD_E_INVAL for NULL arrays, T < 1, n_heads or n_kv_heads < 1, n_axes outside
+ * Errors: SSD_E_INVAL for NULL arrays, T outside [1, 2^25), n_heads or n_kv_heads < 1, n_axes outside
  * [1, 4], a negative section, half = 0, 2 half > head_dim, head_dim > 1024, a row
  * length below its heads, theta not a finite number > 0.
  */
@@ -525,7 +525,8 @@ ssd_status ssd_rope_axes(const ssd_rope_params* params, int32_t T, const void* q
  * Values are rounded to nearest, ties to even; infinities become the largest
  * code, NaN becomes 0.  Codes behind the run stay as they were.
  * Errors: SSD_E_INVAL for NULL arrays, a bad cache, n_rows < 0, a row length below
- * n_kv_heads * head_dim, an unknown dtype.
+ * n_kv_heads * head_dim, an unknown dtype, more rows and heads than one launch takes
+ * (n_kv_heads up to 2^13 and n_rows * n_kv_heads below 2^28 always fit).
  */
 typedef struct {
   int32_t dtype, n_rows;

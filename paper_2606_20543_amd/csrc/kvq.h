@@ -356,15 +356,17 @@ __global__ __launch_bounds__(256) void kvq_append_kernel(KvqAppendArgs a) {
   }
 }
 
+// Rows that a workgroup looks at: four while that makes few enough workgroups (each row may start a run, a
+// step of single tokens), up to 64 for long prompts, where one in a block's rows does.  64 single
+// tokens: 7.4 us a call with windows of 4, 16 with 16, 55 with 64; 16 prompts of up to 2048 rows: 116, 54, 41.
+int kvq_append_window(int n_rows) { return std::max(4, std::min(64, n_rows / 1024 * 4)); }
+
 void kvq_append(KvqAppendArgs a, hipStream_t st) {
   const int es = a.bf16 ? 2 : 4;
   // 16-byte loads, and 32 bits for an offset within a run (16 prompts of up to 2048 rows: 36 us, 59 by elements)
   a.vec_k = (((uintptr_t)a.k | a.ld_k * es) & 15) == 0 && a.ld_k < (1 << 22);
   a.vec_v = (((uintptr_t)a.v | a.ld_v * es) & 15) == 0 && a.ld_v < (1 << 22);
-  // Rows that a workgroup looks at: four while that makes few enough workgroups (each row may start a run, a
-  // step of single tokens), up to 64 for long prompts, where one in a block's rows does.  64 single
-  // tokens: 7.4 us a call with windows of 4, 16 with 16, 55 with 64; 16 prompts of up to 2048 rows: 116, 54, 41.
-  a.window = std::max(4, std::min(64, a.n_rows / 1024 * 4));
+  a.window = kvq_append_window(a.n_rows);
   const dim3 grid((unsigned)((a.n_rows + a.window - 1) / a.window) * a.Hkv * 2);
   const bool two = a.T * a.D > 64 * 128;
   auto kernel = a.bf16 ? two ? kvq_append_kernel<uint16_t, 2> : kvq_append_kernel<uint16_t, 1>

@@ -190,7 +190,7 @@ ssd_status ssd_rope_axes(const ssd_rope_params* p, int32_t T, const void* q, con
                          void* q_out, void* k_out, void* stream) {
   g_err.clear();
   if (!p || !q || !k || !positions || !q_out || !k_out) return fail(SSD_E_INVAL, "NULL argument");
-  if (T < 1) return fail(SSD_E_INVAL, "T = %d must be positive", T);
+  if (T < 1 || T >= 1 << 25) return fail(SSD_E_INVAL, "T = %d outside [1, 2^25)", T);
   if (!dtype_ok(p->dtype)) return fail(SSD_E_INVAL, "unknown dtype");
   if (p->n_heads < 1 || p->n_kv_heads < 1 || p->n_heads > 65535 || p->n_kv_heads > 65535)
     return fail(SSD_E_INVAL, "n_heads and n_kv_heads must lie in [1, 65535]");
@@ -248,6 +248,8 @@ ssd_status ssd_kvq_append(const ssd_kvq_cache* c, const ssd_kvq_append_params* p
   if (p->n_rows < 0) return fail(SSD_E_INVAL, "n_rows = %d is negative", p->n_rows);
   const int64_t cols = (int64_t)c->n_kv_heads * c->head_dim;
   if (p->ld_k < cols || p->ld_v < cols) return fail(SSD_E_INVAL, "row lengths must be at least n_kv_heads * head_dim");
+  if ((int64_t)(p->n_rows / kvq_append_window(p->n_rows) + 1) * c->n_kv_heads * 2 >= 1 << 24)
+    return fail(SSD_E_INVAL, "n_rows = %d of %d heads: more than a launch takes", p->n_rows, c->n_kv_heads);
   if (p->n_rows == 0) return SSD_OK;
   if (!slots || !k || !v || !c->k || !c->v || !c->k_exp || !c->v_exp) return fail(SSD_E_INVAL, "NULL argument");
   const size_t es = p->dtype == SSD_BF16 ? 2 : 4, n = p->n_rows;

@@ -484,6 +484,7 @@ struct KvqAppendArgs {
   size_t ld_k, ld_v;
   int vec_k, vec_v, window;  // the plan (kvq.h)
 };
+int kvq_append_window(int n_rows);
 void kvq_append(KvqAppendArgs a, hipStream_t st);
 struct KvqAttnArgs {
   const uint8_t *kc, *vc, *ke, *ve;

@@ -479,6 +479,76 @@ def test_attention_in_place_and_stale_nan(dev):
     assert np.array_equal(again[~live], q[~live])
 
 
+class Raw:
+    """Device memory whose contents nobody reads before they are written."""
+
+    def __init__(self, nbytes):
+        p = ctypes.c_void_p()
+        assert G.DeviceArray.hip().hipMalloc(ctypes.byref(p), nbytes) == 0
+        self.ptr = p.value
+
+    def put(self, at, host):
+        host = np.ascontiguousarray(host)
+        assert G.DeviceArray.hip().hipMemcpy(self.ptr + at, host.ctypes.data, host.nbytes, 1) == 0
+
+    def get(self, at, shape, dtype):
+        out = np.empty(shape, dtype)
+        assert G.DeviceArray.hip().hipDeviceSynchronize() == 0
+        assert G.DeviceArray.hip().hipMemcpy(out.ctypes.data, self.ptr + at, out.nbytes, 2) == 0
+        return out
+
+    def free(self):
+        assert G.DeviceArray.hip().hipFree(self.ptr) == 0
+
+
+@pytest.mark.parametrize("fresh,hint", [(1, 700), (64, 4352), (80, 4352)])
+def test_offsets_past_32_bits(dev, fresh, hint):
+    """Blocks behind the first 4 GiB of the codes, and rows of queries that far apart: the bits that a small cache and
+    close rows give."""
+    rng = np.random.default_rng(fresh)
+    B, heads, kv, D, block, few = 8, 32, 8, 128, 128, 40
+    many = 2 ** 32 // (kv * D * block) + few
+    lens = np.array([fresh + int(x) for x in rng.integers(0, 500, B)], np.int32)
+    width = -(-hint // block)
+    need = [-(-int(x) // block) for x in lens]
+    assert sum(need) <= few
+    table, at = np.full((B, width), -1, np.int32), 0
+    for b in range(B):
+        table[b, :need[b]] = range(at, at + need[b])
+        at += need[b]
+    slots = np.concatenate([table[b, np.arange(x) // block] * block + np.arange(x) % block for b, x in enumerate(lens)])
+    n, cols, rows = len(slots), kv * D, B * fresh
+    k, _ = typed(rng.standard_normal((n, cols)), "bf16")
+    v, _ = typed(rng.standard_normal((n, cols)), "bf16")
+    q, _ = typed(rng.standard_normal((rows, heads * D)), "bf16")
+    cu, dl, dk, dv = dev(np.arange(0, rows + 1, fresh).astype(np.int32)), dev(lens), dev(k), dev(v)
+    outs, keep = [], []
+    for blocks, shift, ld in ((few, 0, heads * D), (many, many - few, 2 ** 32 // (2 * (rows - 1)) // 8 * 8 + 64)):
+        mem = [Raw(blocks * kv * block * D) for _ in range(2)] + [Raw(blocks * kv) for _ in range(2)] + [Raw(rows * ld * 2) for _ in range(2)]
+        keep += mem
+        c = ssd.ssd_kvq_cache(*[x.ptr for x in mem[:4]], blocks, block, kv, D)
+        ssd.ssd_kvq_append(c, ssd.ssd_kvq_append_params(ssd.SSD_BF16, n, cols, cols), dev((slots + shift * block).astype(np.int32)).ptr,
+                           dk.ptr, dv.ptr)
+        for r in range(rows):
+            mem[4].put(r * ld * 2, q[r])
+        p = ssd.ssd_kvq_attn_params(ssd.SSD_BF16, B, rows, heads, fresh, hint, width, ld, ld, D ** -0.5, 0)
+        p.workspace_bytes = ssd.ssd_kvq_workspace(c, p)
+        work = dev(np.zeros(max(16, p.workspace_bytes), np.uint8))
+        ssd.ssd_kvq_attention(c, p, mem[4].ptr, cu.ptr, dl.ptr, dev(np.where(table < 0, -1, table + shift).astype(np.int32)).ptr,
+                              mem[5].ptr, work.ptr)
+        outs.append([np.stack([mem[5].get(r * ld * 2, heads * D, np.uint16) for r in range(rows)])] +
+                    [mem[i].get(shift * kv * block * D, few * kv * block * D, np.uint8).reshape(few, kv, -1)[:at] for i in range(2)] +
+                    [mem[i].get(shift * kv, (few, kv), np.uint8)[:at] for i in (2, 3)])
+    for x in keep:
+        x.free()
+    assert np.array_equal(outs[0][0], outs[1][0])
+    full = np.zeros((at, block), bool)  # (codes behind a request's end were never written)
+    full.reshape(-1)[slots] = True
+    for i, tokens in ((1, lambda a: a.reshape(at, kv, block, D).transpose(0, 2, 1, 3)), (2, lambda a: a.reshape(at, kv, D, block).transpose(0, 3, 1, 2))):
+        assert np.array_equal(tokens(outs[0][i])[full], tokens(outs[1][i])[full])
+    assert np.array_equal(outs[0][3], outs[1][3]) and np.array_equal(outs[0][4], outs[1][4])
+
+
 # ---------------------------------------------------------------- sampling
 def run_sample(dev, logits, u, V, ld, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, rows=None):
     R = len(u)

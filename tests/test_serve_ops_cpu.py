@@ -84,6 +84,7 @@ def test_rope_refusals(lib):
                      (dict(ld_q=255), "row lengths"), (dict(ld_k_out=1), "row lengths"), (dict(ld_q_out=300), "in place")):
         refused(ssd.ssd_rope_axes, [change(p, **kw), 3] + a, word)
     refused(ssd.ssd_rope_axes, [p, 0] + a, "T = 0")
+    refused(ssd.ssd_rope_axes, [p, 2 ** 25] + a, "T = 33554432")
     for i in range(5):
         refused(ssd.ssd_rope_axes, [p, 3] + a[:i] + [None] + a[i + 1:], "NULL")
 
@@ -97,7 +98,7 @@ def test_append_refusals(lib):
     c, p = ssd.ssd_kvq_cache(**CACHE), ssd.ssd_kvq_append_params(ssd.SSD_F32, 5, 128, 128)
     for kw, word in BAD_CACHE:
         refused(ssd.ssd_kvq_append, (change(c, **kw), p, X, X, X), word)
-    for kw, word in ((dict(dtype=2), "dtype"), (dict(n_rows=-1), "n_rows"), (dict(ld_k=127), "row lengths"), (dict(ld_v=0), "row lengths")):
+    for kw, word in ((dict(dtype=2), "dtype"), (dict(n_rows=-1), "n_rows"), (dict(n_rows=2 ** 29), "launch"), (dict(ld_k=127), "row lengths"), (dict(ld_v=0), "row lengths")):
         refused(ssd.ssd_kvq_append, (c, change(p, **kw), X, X, X), word)
     for i in range(3):
         refused(ssd.ssd_kvq_append, [c, p] + [X] * i + [None] + [X] * (2 - i), "NULL")
