@@ -1,6 +1,7 @@
 """The serving operators (ssd_kvq_*, ssd_rope_axes, ssd_sample_logits) against plain 64-bit implementations
 (tests/serve_util.py), at the sizes, masks and strides where they can go wrong."""
 import ctypes
+from concurrent.futures import ThreadPoolExecutor
 
 import numpy as np
 import pytest
@@ -786,6 +787,47 @@ def test_captured_step_replays(dev):
         if graph:
             hip.hipGraphDestroy(graph)
         hip.hipStreamDestroy(stream)
+
+
+def test_two_streams_at_once(dev):
+    """Two threads, each with a stream, arrays and a workspace of its own, on one card: what each gives alone."""
+    hip = G.DeviceArray.hip()
+    heads, kv, D, block, V = 32, 8, 128, 64, 20000
+    streams = [ctypes.c_void_p() for _ in range(2)]
+    calls, outs = [], []
+    for i, reqs in enumerate(([(1500, 64), (903, 50), (64, 64), (705, 33), (1000, 40), (600, 64), (300, 60), (1200, 64)],
+                              [(2000, 1), (900, 1), (3000, 1), (64, 1)])):
+        assert hip.hipStreamCreate(ctypes.byref(streams[i])) == 0
+        rng = np.random.default_rng(70 + i)
+        _, _, _, (c, p, dq, dcu, dl, dt, do, work, *_) = attend_case(dev, rng, "bf16", heads, kv, D, block, reqs, width=68, max_len=4352)
+        B, R = len(reqs), 6
+        ps = ssd.ssd_sample_params(vocab=V, ld=V, temperature=1.0, top_k=500, top_p=0.9)
+        logits, u = dev(logit_rows(rng, R, V)), dev(rng.random(R).astype(np.float32))
+        tok, prob = dev(np.zeros(R, np.int32)), dev(np.zeros(R, np.float32))
+        ps_rope = ssd.ssd_rope_params(heads, heads, D, ssd.SSD_BF16, 3, (16, 24, 24), p.ld_q, p.ld_out, p.ld_q, p.ld_q, 1e4)
+        pos = dev(rng.integers(0, 5000, 3 * p.n_rows).astype(np.int32))
+        qo, ko = dev(np.zeros((p.n_rows, p.ld_q), np.uint16)), dev(np.zeros((p.n_rows, p.ld_q), np.uint16))
+
+        def call(c=c, p=p, a=(dq, dcu, dl, dt, do, work), ps=ps, b=(logits, u, tok, prob), pr=ps_rope, e=(pos, qo, ko), st=streams[i]):
+            ssd.ssd_kvq_attention(c, p, *[x.ptr for x in a], st.value)
+            ssd.ssd_rope_axes(pr, p.n_rows, a[0].ptr, a[4].ptr, *[x.ptr for x in e], st.value)
+            ssd.ssd_sample_logits(ps, R, *[x.ptr for x in b], st.value)
+        calls.append(call)
+        outs.append((do, qo, ko, tok, prob))
+    try:
+        alone = []
+        for f, o in zip(calls, outs):
+            f()
+            alone.append([x.numpy() for x in o])
+        with ThreadPoolExecutor(2) as pool:
+            for _ in range(3):
+                list(pool.map(lambda f: [f() for _ in range(10)], calls))
+                for o, want in zip(outs, alone):
+                    assert all(np.array_equal(x.numpy(), w) for x, w in zip(o, want))
+    finally:
+        for st in streams:
+            if st:
+                hip.hipStreamDestroy(st)
 
 
 def test_refused_arrays(dev):
