@@ -17,11 +17,11 @@
 // in registers up to 32768 codes.
 //
 // Four rows of 16384 codes with top-k and top-p: 20.5 us a call, a chain of some fifteen
-// barriers in one workgroup each.  512 rows of 32768, settings of their own: 84 to 88 us (67 MB,
-// 13 us at the rate of a large copy; two rows a CU one after the other): reading and the draw 37, the
-// codes' counts 22 more, the sums of their weights 15, both in atomics on shared memory, one
-// a code, and the float64 exponentials.  Rows that start on 16 bytes are read by four codes
-// (89 us, 106 by single ones).
+// barriers in one workgroup each.  512 rows of 32768, settings of their own: 75 us (67 MB, 13 us
+// at the rate of a large copy; two rows a CU one after the other).  With the same settings in all rows:
+// reading and the draw 37, a top-k 21 more, a top-p 26, both 39: atomics on shared memory, one
+// or two a code at about a lane and cycle, and the float64 exponentials.  Rows that start on
+// 16 bytes are read by four codes (17 us less).
 #pragma once
 
 namespace ssd {
@@ -413,12 +413,23 @@ __global__ __launch_bounds__(LS_T) void sample_logits_kernel(SampleArgs a) {
   const double u = a.u[r];
   const LsRow<NG> row(a.logits + (size_t)r * a.ld, V);
   if (tid < LS_POW) sh.pow2[tid] = LS_ONE * exp2((double)tid / LS_POW);
-  float mx = -INFINITY;
-  row.each([&](int, const float(&x)[4]) { mx = fmaxf(mx, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]))); });
+  float mx = -INFINITY, mn = INFINITY;  // (the least that can be drawn)
+  row.each([&](int, const float(&x)[4]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      mx = fmaxf(mx, x[e]);
+      mn = fminf(mn, x[e] == -INFINITY ? INFINITY : x[e]);
+    }
+  });
   mx = ls_wave(mx, LsMax{});
-  if (lane == 0) sh.fmx[wave] = mx;
+  mn = ls_wave(mn, LsMin{});
+  if (lane == 0) {
+    sh.fmx[wave] = mx;
+    sh.fmn[wave] = mn;
+  }
   __syncthreads();
   mx = ls_row(sh.fmx[lane & 15], LsMax{});
+  mn = ls_row(sh.fmn[lane & 15], LsMin{});
   if (mx == -INFINITY || !(T > 0.0)) {  // nothing to draw, or the largest (its lowest code)
     int am = 0x7fffffff;
     row.again([&](int v, const float(&x)[4]) {
@@ -444,7 +455,7 @@ __global__ __launch_bounds__(LS_T) void sample_logits_kernel(SampleArgs a) {
   int bi = 0x7fffffff;
   const bool by_k = top_k > 0 && top_k < V, by_p = top_p < 1.0;
   if (by_k || by_p) {
-    const LsBins bins(floor_l, mx);
+    const LsBins bins(fmaxf(floor_l, mn), mx);  // (from floor_l alone: 88 us in place of 75, warm rows share few bins)
     const LsCumul q = ls_histogram(row, wt, bins, by_k, by_p, 0u, 0ull, sh);
     double mass = 0.0;
     if (by_k) {
