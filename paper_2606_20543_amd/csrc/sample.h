@@ -17,7 +17,7 @@
 // in registers up to 32768 codes.
 //
 // Four rows of 16384 codes with top-k and top-p: 20.5 us a call, a chain of some fifteen
-// barriers in one workgroup each.  512 rows of 32768, settings of their own: 75 us (67 MB, 13 us
+// barriers in one workgroup each.  512 rows of 32768, settings of their own: 77 us (67 MB, 13 us
 // at the rate of a large copy; two rows a CU one after the other).  With the same settings in all rows:
 // reading and the draw 37, a top-k 21 more, a top-p 26, both 39: atomics on shared memory, one
 // or two a code at about a lane and cycle, and the float64 exponentials.  Rows that start on

@@ -16,7 +16,7 @@ namespace ssd {
 // so one launch does it with no hand-off between workgroups; several share the rows
 // of the same requests where there are many.  Bound by its
 // launch and three dependent round trips (lengths, table or pool entry, store): 64
-// requests of one new token 7.6 us a call (4.9 the kernel), 2048 of up to 64 7.8 (7.1).
+// requests of one new token 7.6 us a call (5.3 the kernel), 2048 of up to 64 7.7.
 constexpr int SLOT_T = 256, SLOT_SEQS = 8;
 
 __device__ __forceinline__ long long wave_sum_ll(long long v) {
