@@ -231,7 +231,12 @@ __device__ __forceinline__ float kvq_shared_scale(const KvqRun<E>& run, int whic
   __syncthreads();
   const uint32_t top = max(max(red[0], red[1]), max(red[2], red[3]));  // of magnitudes: ordered like their bits
   const int old = (int)red[4], s = max(kvq_exponent(__uint_as_float(top)), old);
-  run.template rescale<256>(which, T, D, old, s, threadIdx.x);
+  if (run.off > 0 && s > old) {  // (the same in the whole workgroup)
+    run.template rescale<256>(which, T, D, old, s, threadIdx.x);
+    // The last word of a dim's older values holds the first new ones too: they are stored, by whichever wave,
+    // once every such word has been written back.
+    __syncthreads();
+  }
   if (threadIdx.x == 0) *run.ep = (uint8_t)s;
   return kvq_pow2(127 - s);
 }

@@ -283,6 +283,62 @@ def test_append_nothing(dev):
     assert_cache(arrs, plain)
 
 
+@pytest.mark.parametrize("dtype,D,block", [("bf16", 128, 64), ("f32", 128, 32), ("bf16", 64, 32), ("f32", 64, 64), ("bf16", 128, 128)])
+@pytest.mark.parametrize("requests,step", [(1, 1), (2, 1), (1, 3), (2, 5), (9, 1)])
+def test_append_where_the_scale_grows(dev, dtype, D, block, requests, step):
+    """A few requests fill a block each from its first token, `step` rows a call: every call finds a larger magnitude, so
+    the older codes of both sides are rounded again while the new ones are stored beside them, in the same words."""
+    rng = np.random.default_rng(block + D + 10 * requests + step)
+    kv, rows = 24, requests * step
+    c, arrs, plain = cache_arrays(dev, rng, requests + 2, kv, block, D)
+    pages = rng.permutation(requests + 2)[:requests]
+    p = ssd.ssd_kvq_append_params(code(dtype), rows, kv * D, kv * D)
+    calls = -(-block // step)
+    growth = np.exp2(12.0 / calls)  # 12 steps of the exponent from first to last
+    raw = [[], []]
+    for i in range(calls):
+        size = growth ** i * (1 + 0.2 * rng.random((rows, kv, 1)))
+        for side in raw:
+            side.append(typed((rng.uniform(-1, 1, (rows, kv, D)) * size).reshape(rows, kv * D), dtype))
+    dk, dv = (dev(np.stack([x[0] for x in side])) for side in raw)
+    slots = np.full((calls, rows), -1, np.int32)
+    for i in range(calls):
+        n = min(step, block - i * step)
+        for b in range(requests):
+            slots[i, b * step:b * step + n] = pages[b] * block + i * step + np.arange(n)
+    ds = dev(slots)
+    es = raw[0][0][0].itemsize
+    for i in range(calls):
+        at = i * rows * kv * D * es
+        ssd.ssd_kvq_append(c, p, ds.ptr + i * rows * 4, dk.ptr + at, dv.ptr + at)
+        plain.append(slots[i], *(side[i][1].reshape(rows, kv, D) for side in raw))
+        if i % 8 == 1 or i == calls - 1:
+            assert_cache(arrs, plain)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,block,off", [(128, 64, 1), (128, 64, 5), (64, 128, 127), (128, 128, 66), (64, 32, 3), (128, 16, 15)])
+def test_append_behind_small_tokens(dev, dtype, D, block, off):
+    """One new token, one call a block, in many blocks whose older tokens have a far smaller scale."""
+    rng = np.random.default_rng(block + off)
+    kv, n_blocks = 16, 60
+    c, arrs, plain = cache_arrays(dev, rng, n_blocks, kv, block, D)
+    for a in arrs[2:]:
+        upload(a, np.full((n_blocks, kv), 118, np.uint8))
+    plain.ke[:], plain.ve[:] = 118, 118
+    (k, kval), (v, vval) = (typed(rng.standard_normal((n_blocks, kv * D)) * 40.0, dtype) for _ in range(2))
+    dk, dv, es = dev(k), dev(v), k.itemsize
+    slots = (np.arange(n_blocks) * block + off).astype(np.int32)
+    ds = dev(slots)
+    p = ssd.ssd_kvq_append_params(code(dtype), 1, kv * D, kv * D)
+    for i in range(n_blocks):
+        ssd.ssd_kvq_append(c, p, ds.ptr + 4 * i, dk.ptr + i * kv * D * es, dv.ptr + i * kv * D * es)
+    for i in range(n_blocks):
+        plain.append(slots[i:i + 1], kval[i:i + 1].reshape(1, kv, D), vval[i:i + 1].reshape(1, kv, D))
+    assert (plain.ve > 118).all()
+    assert_cache(arrs, plain)
+
+
 # ---------------------------------------------------------------- attention
 def attend_case(dev, rng, dtype, heads, kv, D, block, reqs, width=None, extra=0, hide=(), max_q=None, max_len=None,
                 q_scale=1.0, scale=None):
