@@ -550,7 +550,8 @@ ssd_status ssd_kvq_append(const ssd_kvq_cache* cache, const ssd_kvq_append_param
  * Rows of out that belong to no request stay as they were.
  * max_q >= the most rows of a request (rows past it are not computed) and max_len
  * >= the largest len (a hint that splits long contexts; a wrong one costs time only)
- * are the host's bounds.  scale: any finite number (1/sqrt(head_dim) as a rule).
+ * are the host's bounds.  scale: any finite number (1/sqrt(head_dim) as a rule); scores
+ * may be as large as fp32 holds (scale * q k / ln 2 below 3e38 in magnitude).
  * workspace: ssd_kvq_workspace bytes (0: may be NULL), 16-byte aligned, for partial
  * results; its contents do not matter before or after a call, but calls that run
  * at the same time need one each (graphs that may overlap too).

@@ -398,17 +398,23 @@ void kvq_append(KvqAppendArgs a, hipStream_t st) {
 // operand, fp32 ones the sum of three (all 24 bits).  Weights are p = 2^(t - m) in fp32,
 // t the score in the log2 domain.  fp32 calls split them into three bf16 operands like
 // the queries, the values being bf16 with their scale.  bf16 calls have one operand:
-// the weights take the value scale along, p' = 2^(t + e - R), e the value exponent of the
-// key's block and R a running bound of t + e, so that the codes themselves, exact in fp16,
+// the weights take the value scale along, p' = 2^(t - m + e - R), e the value exponent of the
+// key's block and R a running bound of t - m + e, so that the codes themselves, exact in fp16,
 // are the other operand whatever the scales of different blocks are; p' is rounded to fp16,
 // 11 bits where the output has 8.  p' is formed alone, a lane's 16 of a step share e, so l takes
-// their sum times 2^(R - e - m).  m and R follow their maxima lazily: only where a lane
+// their sum times 2^(R - e).  m and R follow their maxima lazily: only where a lane
 // finds one grown by more than 2^8 are the maxima of all lanes taken and the sums rescaled.
+//
+// t - m + e - R is one multiply-add of a product and m - e + R while m is below 2^22.  Beyond, that sum and
+// the rounding of t to fp32 are off by more than the exponent of a weight may be (equal scores of 3e7 gave infinite
+// fp16 weights), so there t is rounded first, as m is, and the small terms join the difference.  Scores may be as large
+// as fp32 holds.
 typedef _Float16 kvq_h8 __attribute__((ext_vector_type(8)));
 typedef _Float16 kvq_h2 __attribute__((ext_vector_type(2)));
 
 constexpr int KVQ_STEP = 64;
-constexpr float KVQ_NONE = -1e30f;  // m and R before the first key
+constexpr float KVQ_NONE = -3.4028234664e38f;  // m before the first key
+constexpr float KVQ_FAR = 4194304.f;           // |m| from which differences are taken first
 constexpr float KVQ_LAZY = 8.f;
 constexpr float KVQ_LIFT = 6.f;     // p' of the largest lies at 2^6 (2^14 before R moves on): fp16 steps of 2^-30 of it
 
@@ -521,6 +527,16 @@ struct KvqWalk {
   }
 };
 
+// a score in the log2 domain, rounded as one number, and what it lies above m: kept apart (fused, the
+// product's rounding would be left over, more than an exponent holds where scores are large)
+__device__ __forceinline__ float kvq_score(float s, float sc) {
+#pragma clang fp contract(off)
+  return s * sc;
+}
+__device__ __forceinline__ float kvq_above(float s, float sc, float m) {
+#pragma clang fp contract(off)
+  return s * sc - m;
+}
 // larger of two scores (the median with infinity: fmaxf would first quiet signalling NaNs, an instruction an operand)
 __device__ __forceinline__ float kvq_max(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, INFINITY); }
 // largest over the four lane groups, in every lane
@@ -536,13 +552,15 @@ struct KvqRows {
   bf16x8 q[QT][PL][D / 32];
   floatx4 O[QT][D / 16];
   float m[QT], R[QT], l[QT];
+  bool far[QT];    // |m| past KVQ_FAR in a lane (the same in the wave)
   int pos[QT];  // last position that this lane's row sees (-1: none)
 
   __device__ __forceinline__ void start() {
 #pragma unroll
     for (int i = 0; i < QT; ++i) {
-      m[i] = R[i] = KVQ_NONE;
-      l[i] = 0.f;
+      m[i] = KVQ_NONE;
+      R[i] = l[i] = 0.f;
+      far[i] = false;
 #pragma unroll
       for (int dt = 0; dt < D / 16; ++dt) O[i][dt] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
@@ -597,7 +615,7 @@ struct KvqRows {
   }
 
   // what takes the sums from R (and the codes' exponents) to m
-  __device__ __forceinline__ float to_m(int i) const { return HALF ? exp2f(R[i] - m[i] - 127.f) : 1.f; }
+  __device__ __forceinline__ float to_m(int i) const { return HALF ? exp2f(R[i] - 127.f) : 1.f; }
 
   // one step: keys j0 .. j0 + 63, their operands from src, iev the value exponent of this lane's keys
   // (scored(): the key operands are free)
@@ -638,27 +656,41 @@ struct KvqRows {
       float x = S[i][0][0];
 #pragma unroll
       for (int j = 1; j < 16; ++j) x = kvq_max(x, S[i][j >> 2][j & 3]);
-      x *= sc;
-      // (a block that is not there: an exponent that leaves the factor 1; its scores are -inf)
-      float ev = !HALF ? 0.f : !MASK || iev >= 0 ? (float)iev : R[i] - m[i];
-      if (__any(x > m[i] + KVQ_LAZY || (HALF && x + ev > R[i] + (KVQ_LAZY + KVQ_LIFT)))) {
-        const float mn = fmaxf(m[i], kvq_max_groups(x)), rn = HALF ? fmaxf(R[i], kvq_max_groups(x + ev) - KVQ_LIFT) : mn;
-        const float fr = exp2f(R[i] - rn);
-        l[i] *= exp2f(m[i] - mn);
+      x = kvq_score(x, sc);
+      // e - R (0 for a block that is not there, whose scores are -inf)
+      float ev = 0.f;
+      if (HALF && (!MASK || iev >= 0)) ev = (float)iev - R[i];
+      if (__builtin_expect(far[i] | (__ballot(x > m[i] + (HALF ? fminf(KVQ_LAZY, KVQ_LAZY + KVQ_LIFT - ev) : KVQ_LAZY)) != 0), 0)) {
+        const float mn = fmaxf(m[i], kvq_max_groups(x)), down = m[i] - mn;
+        float fr = down;
+        if constexpr (HALF) {
+          const float up = fmaxf(down, kvq_max_groups(x - mn + ev) - KVQ_LIFT);  // R's move
+          R[i] += up;
+          if (!MASK || iev >= 0) ev -= up;
+          fr -= up;
+        }
+        fr = exp2f(fr);
+        l[i] *= exp2f(down);
 #pragma unroll
         for (int dt = 0; dt < D / 16; ++dt) O[i][dt] *= fr;
         m[i] = mn;
-        R[i] = rn;
-        if (HALF && MASK && iev < 0) ev = rn - mn;
+        far[i] = __any(fabsf(mn) > KVQ_FAR && mn > KVQ_NONE);
+        if (far[i]) {
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) S[i][t][e] = kvq_above(S[i][t][e], sc, mn);
+        }
       }
-      const float off = HALF ? ev - R[i] : -m[i];
+      // exponents of p: S f + at; of p': S f + off
+      const float f = far[i] ? 1.f : sc, at = far[i] ? 0.f : -m[i], off = ev + at;
       float ls = 0.f;
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         float p[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          p[e] = __builtin_amdgcn_exp2f(fmaf(S[i][t][e], sc, off));
+          p[e] = __builtin_amdgcn_exp2f(fmaf(S[i][t][e], f, off));
           ls += p[e];
         }
 #pragma unroll
@@ -675,16 +707,15 @@ struct KvqRows {
           }
       }
       if constexpr (HALF) {
-        const float up = R[i] - m[i] - ev;  // from p' to p
-        ls *= __builtin_amdgcn_exp2f(up);
+        ls *= __builtin_amdgcn_exp2f(-ev);  // from p' to p
         // values 2^60 below what the largest p' stands for (blocks of zeros): p' may have
         // left fp32's range where p has not
-        if (__any(up > 60.f)) {
+        if (__any(ev < -60.f)) {
           float ps = 0.f;
 #pragma unroll
           for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) ps += __builtin_amdgcn_exp2f(fmaf(S[i][t][e], sc, -m[i]));
+            for (int e = 0; e < 4; ++e) ps += __builtin_amdgcn_exp2f(fmaf(S[i][t][e], f, at));
           ls = ps;
         }
       }

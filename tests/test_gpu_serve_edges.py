@@ -1,0 +1,87 @@
+"""The serving operators at the edges of what their calls allow: scores and magnitudes near the ends of fp32, row offsets
+that leave the arrays, very many requests, unaligned outputs, errors that others left behind."""
+import ctypes
+import dataclasses
+
+import numpy as np
+import pytest
+
+import paper_2606_20543_amd as ssd
+import synth
+from tests import gpu_util as G
+from tests import serve_util as S
+from tests.test_gpu_serve_ops import Dev, cache_arrays, code, slot_case, typed, upload, values
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture
+def dev():
+    d = Dev()
+    yield d
+    d.free()
+
+
+def attend(dev, c, dtype, q, cu, lens, table, scale, max_q=None, max_len=None, heads=None, in_place=False):
+    """One call on rows of q [n][heads][D] as the device holds them; rows that it leaves alone hold 77."""
+    n, heads, D = q.shape
+    p = ssd.ssd_kvq_attn_params(code(dtype), len(lens), n, heads, max_q or max(1, int(np.diff(cu).max())),
+                                max_len or max(1, int(max(lens))), table.shape[1], heads * D, heads * D, scale, 0)
+    p.workspace_bytes = ssd.ssd_kvq_workspace(c, p)
+    work = dev(np.full(max(16, p.workspace_bytes), 0xFF, np.uint8))  # NaN bit patterns
+    out = dev(typed(np.full((n, heads, D), 77.0), dtype)[0])
+    i32 = lambda x: dev(np.asarray(x, np.int32)).ptr  # noqa: E731
+    ssd.ssd_kvq_attention(c, p, dev(q).ptr, i32(cu), i32(lens), i32(table), out.ptr, work.ptr)
+    return values(out, dtype)
+
+
+# dtype, heads, kv, D, block, table width, (len, rows) of every request, whether the hint is the table's width
+# (a wide table splits the keys into shares; bf16 calls with many rows of many requests split the rows between waves)
+EQUAL = [("f32", 4, 4, 64, 16, 20, [(300, 3), (1, 1), (65, 65)], False), ("f32", 8, 2, 128, 64, 90, [(500, 1), (90, 2)], True),
+         ("bf16", 16, 16, 128, 32, 13, [(412, 1), (70, 3)], False), ("bf16", 8, 2, 64, 128, 60, [(1000, 1), (1, 1), (200, 20)], True),
+         ("bf16", 32, 8, 128, 64, 68, [(400, 64), (100, 50), (64, 64), (3, 3), (305, 33), (129, 1), (500, 40), (80, 64)], True),
+         ("bf16", 32, 8, 64, 16, 272, [(300, 64), (200, 50), (64, 64), (63, 63), (205, 33), (129, 1), (300, 40), (2, 2)], True)]
+
+
+@pytest.mark.parametrize("dtype,heads,kv,D,block,width,reqs,wide", EQUAL)
+@pytest.mark.parametrize("log2,negative", [(12, False), (21, False), (25, True), (28, False), (33, True), (66, False), (101, False),
+                                           (126, False), (126, True)])
+def test_attention_scores_of_any_size(dev, dtype, heads, kv, D, block, width, reqs, wide, log2, negative):
+    """Keys of all ones or all minus ones under equal queries: scores +-1.5 2^log2, exact and equal but for their sign, the
+    low ones first.  Of what a row sees, the larger scores share the weight: the mean of their values.
+
+    Weights of equal scores are equal to fp32's roundings: the sums are off by (n + 16) 2^-24 of the magnitudes, fp16
+    weights of bf16 calls by 2^-11, the result by its rounding."""
+    rng = np.random.default_rng(log2 + D)
+    B, lens = len(reqs), [r[0] for r in reqs]
+    cu = np.concatenate([[0], np.cumsum([r[1] for r in reqs])])
+    need = [-(-x // block) for x in lens]
+    n_blocks = sum(need) + 1
+    table, at, ids = np.full((B, width), -1, np.int32), 0, rng.permutation(n_blocks)
+    for b in range(B):
+        table[b, :need[b]] = ids[at:at + need[b]]
+        at += need[b]
+    c, arrs, plain = cache_arrays(dev, rng, n_blocks, kv, block, D)
+    low = [np.concatenate([np.ones(min(70, x // 2 + 1), bool), rng.random(max(0, x - min(70, x // 2 + 1))) < 0.5]) for x in lens]
+    k = np.full((n_blocks, kv, block, D), 0x38, np.uint8)  # 1
+    for b in range(B):
+        for p in np.nonzero(low[b])[0]:
+            k[table[b, p // block], :, p % block] = 0xB8
+    e = log2 // 2
+    upload(arrs[0], k)
+    upload(arrs[2], np.full((n_blocks, kv), 127 + e, np.uint8))
+    q = typed(np.full((int(cu[-1]), heads, D), (-1.5 if negative else 1.5) * 2.0 ** (log2 - e - D.bit_length() + 1)), dtype)[0]
+    # (scale 1: 1.5 2^(log2 - e) / D, D times, by 2^e; a negative scale gives the same scores)
+    got = attend(dev, c, dtype, q, cu, lens, table, -1.0 if negative else 1.0, max_len=width * block if wide else None)
+    g, u = heads // kv, 2.0 ** -24
+    V = plain.v * np.exp2(plain.ve - 127.0)[:, :, None, None]  # [blocks][kv][block][D]
+    for b in range(B):
+        pg, at = table[b, np.arange(lens[b]) // block], np.arange(lens[b]) % block
+        for i in range(reqs[b][1]):
+            seen = np.arange(lens[b]) <= lens[b] - reqs[b][1] + i
+            most = seen & ~low[b] if (seen & ~low[b]).any() else seen
+            v = V[pg[most], :, at[most]]  # [n][kv][D]
+            want, mag = (np.repeat(x.mean(0), g, 0) for x in (v, np.abs(v)))
+            tol = mag * ((lens[b] + 16) * u + (2.0 ** -11 if dtype == "bf16" else 0)) + np.abs(want) * (2.0 ** -8 if dtype == "bf16" else 0)
+            worst = float((np.abs(got[cu[b] + i] - want) - tol).max())
+            assert worst <= 0, (b, i, worst)
