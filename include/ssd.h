@@ -550,14 +550,14 @@ ssd_status ssd_kvq_append(const ssd_kvq_cache* cache, const ssd_kvq_append_param
  * Rows of out that belong to no request stay as they were.
  * max_q >= the most rows of a request (rows past it are not computed) and max_len
  * >= the largest len (a hint that splits long contexts; a wrong one costs time only)
- * are the host's bounds.  scale: any finite number (1/sqrt(head_dim) as a rule); scores
+ * are the host's bounds.  scale: any number below 2.3e38 in magnitude (1/sqrt(head_dim) as a rule); scores
  * may be as large as fp32 holds (scale * q k / ln 2 below 3e38 in magnitude).
  * workspace: ssd_kvq_workspace bytes (0: may be NULL), 16-byte aligned, for partial
  * results; its contents do not matter before or after a call, but calls that run
  * at the same time need one each (graphs that may overlap too).
  * Errors: SSD_E_INVAL for NULL arrays, a bad cache, n_seqs, n_rows, max_q, max_len or
  * table_width < 1, n_heads no multiple of n_kv_heads, a row length below n_heads *
- * head_dim, an unknown dtype, a non-finite scale, too small a workspace,
+ * head_dim, an unknown dtype, a scale that is no such number, too small a workspace,
  * n_seqs * max_q * n_heads of 2^31 or more, n_seqs * n_kv_heads * ceil(max_q * n_heads
  * / n_kv_heads / 16) of 2^24 or more, a table of more than 2^30 positions.
  */

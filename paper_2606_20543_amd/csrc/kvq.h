@@ -1164,11 +1164,12 @@ void kvq_attention(KvqAttnArgs a, hipStream_t st) {
   kvq_attn_plan(a);
   a.part_o = (float*)a.workspace;
   a.part_s = (float2*)(a.part_o + kvq_part_rows(a) * a.D);
-  // a negative scale turns the queries' signs; scores of a zero one are all 0 (not 0 * -inf where a key is hidden)
-  a.neg = a.scale < 0.f;
+  // a negative scale turns the queries' signs
+  a.neg = a.scale < 0.0;
   // rows start on 16 bytes, heads then do (8 x 64 rows of 32 heads: 46 us, 51 by elements)
   a.vec = (((uintptr_t)a.q | a.ld_q * (a.bf16 ? 2 : 4)) & 15) == 0;
-  a.scale_log2 = fmaxf(fabsf(a.scale) * 1.4426950408889634f, 1e-37f);
+  // a zero scale: the smallest number in its place, whose scores are below 2^-21 (0 * -inf is none where a key is hidden)
+  a.scale_log2 = std::max(kvq_scale_log2(a.scale), 0x1p-149f);
   if (a.bf16) {
     if (a.D == 128) kvq_launch<uint16_t, 128>(a, st);
     else kvq_launch<uint16_t, 64>(a, st);

@@ -111,7 +111,7 @@ ssd_status attn_sizes(const ssd_kvq_cache* c, const ssd_kvq_attn_params* p, KvqA
     return fail(SSD_E_INVAL, "table_width * block must be at most 2^30 positions");
   const int64_t cols = (int64_t)p->n_heads * c->head_dim;
   if (p->ld_q < cols || p->ld_out < cols) return fail(SSD_E_INVAL, "row lengths must be at least n_heads * head_dim");
-  if (!std::isfinite(p->scale) || !std::isfinite((float)p->scale)) return fail(SSD_E_INVAL, "scale must be finite");
+  if (!std::isfinite(kvq_scale_log2(p->scale))) return fail(SSD_E_INVAL, "scale must be finite, below 2.3e38 in magnitude");
   a = KvqAttnArgs{};
   a.n_blocks = c->n_blocks;
   a.T = c->block;
@@ -126,7 +126,7 @@ ssd_status attn_sizes(const ssd_kvq_cache* c, const ssd_kvq_attn_params* p, KvqA
   a.bf16 = p->dtype == SSD_BF16;
   a.ld_q = (size_t)p->ld_q;
   a.ld_o = (size_t)p->ld_out;
-  a.scale = (float)p->scale;
+  a.scale = p->scale;
   return SSD_OK;
 }
 

@@ -37,6 +37,7 @@
 #include <limits.h>
 #include <stdint.h>
 
+#include <cmath>
 #include <vector>
 
 #include "../../include/ssd.h"
@@ -494,7 +495,7 @@ struct KvqAttnArgs {
   void* o;
   size_t ld_q, ld_o;
   const int *cu, *lens, *table;
-  float scale;
+  double scale;
   void* workspace;
   // the plan (kvq.h): row groups, key shares, partial results in the workspace
   int by_rows, qt, groups, group_rows, rows_pad, nsplit, chunk, neg, vec;
@@ -502,6 +503,7 @@ struct KvqAttnArgs {
   float* part_o;   // [B][Hkv][nsplit][rows_pad][D], relative to the row's maximum
   float2* part_s;  // [B][Hkv][nsplit][rows_pad] (maximum, log2 domain; sum)
 };
+inline float kvq_scale_log2(double scale) { return (float)(std::fabs(scale) * 1.4426950408889634); }
 size_t kvq_attn_workspace(KvqAttnArgs a);  // bytes
 void kvq_attention(KvqAttnArgs a, hipStream_t st);
 

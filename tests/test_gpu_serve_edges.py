@@ -85,3 +85,31 @@ def test_attention_scores_of_any_size(dev, dtype, heads, kv, D, block, width, re
             tol = mag * ((lens[b] + 16) * u + (2.0 ** -11 if dtype == "bf16" else 0)) + np.abs(want) * (2.0 ** -8 if dtype == "bf16" else 0)
             worst = float((np.abs(got[cu[b] + i] - want) - tol).max())
             assert worst <= 0, (b, i, worst)
+
+
+@pytest.mark.parametrize("dtype,heads,kv,D,block,width,reqs,wide", EQUAL)
+@pytest.mark.parametrize("scale,q_scale", [(0.0, 1.0), (-0.0, 1e34), (0.0, 1e34), (1e-40, 1e34), (-1e-42, 1e36), (2e-45, 1e3)])
+def test_attention_tiny_scales(dev, dtype, heads, kv, D, block, width, reqs, wide, scale, q_scale):
+    """A scale of zero gives every seen key the same weight, one below fp32's normal range its own; hidden blocks stay hidden."""
+    rng = np.random.default_rng(D + block)
+    B, lens = len(reqs), [r[0] for r in reqs]
+    cu = np.concatenate([[0], np.cumsum([r[1] for r in reqs])])
+    need = [-(-x // block) for x in lens]
+    c, arrs, plain = cache_arrays(dev, rng, sum(need) + 1, kv, block, D)
+    table, at, ids = np.full((B, width), -1, np.int32), 0, rng.permutation(sum(need) + 1)
+    for b in range(B):
+        table[b, :need[b]] = ids[at:at + need[b]]
+        at += need[b]
+    table[0, need[0] // 2] = -1
+    table[B - 1, 0] = 10 ** 6
+    q, val = typed(rng.standard_normal((int(cu[-1]), heads, D)) * q_scale, dtype)
+    got = attend(dev, c, dtype, q, cu, lens, table, scale, max_len=width * block if wide else None)
+    want, tol = S.attention(plain, val, cu, lens, table, scale, dtype == "bf16")
+    # the scale (its product with log2 e) is one of fp32: off by at most a step of 2^-149 below the normal range, and so
+    # scores by that times q.k; exp of that less one, twice, of sum p |v|, which is at most the largest |v|
+    top = 448.0 * np.exp2(plain.ve.max() - 127.0)
+    qk = np.abs(val).sum(2).max() * np.abs(plain.k * np.exp2(plain.ke - 127.0)[:, :, None, None]).max()
+    d = qk * (2.0 ** -148 if abs(scale) < 2.0 ** -126 else 0)
+    assert d < 1e-3
+    worst = float((np.abs(got - want) - tol - 4 * d * top).max())
+    assert worst <= 0
