@@ -523,7 +523,9 @@ ssd_status ssd_rope_axes(const ssd_rope_params* params, int32_t T, const void* q
  * codes are rounded again to the new scale (exact unless they leave e4m3's normal
  * range).  A run at offset 0 sets the exponent anew: what the block held is gone.
  * Values are rounded to nearest, ties to even; infinities become the largest
- * code, NaN becomes 0.  Codes behind the run stay as they were.
+ * code, NaN becomes 0.  (The largest code is 448; at the exponent 247, of magnitudes
+ * from 448 * 2^119 on, it is 240, since more would stand for what fp32 does not hold.)
+ * Codes behind the run stay as they were.
  * Errors: SSD_E_INVAL for NULL arrays, a bad cache, n_rows < 0, a row length below
  * n_kv_heads * head_dim, an unknown dtype, more rows and heads than one launch takes
  * (n_kv_heads up to 2^13 and n_rows * n_kv_heads below 2^28 always fit).

@@ -6,8 +6,8 @@
 // block of T tokens and a head share one power-of-two scale 2^(s - 127) for its
 // keys and one for its values.  A power of two keeps the three fraction bits
 // of every code whatever the scale (an e4m3 code is a floating number: another
-// factor would buy nothing), makes a code times its scale exact in bf16, and
-// makes a rescaled code exact as long as it stays normal.
+// factor would buy nothing), makes a code times its scale exact in bf16 (but what lies
+// below 2^-133), and makes a rescaled code exact as long as it stays normal.
 #pragma once
 
 #include "ssd_internal.h"
@@ -29,11 +29,18 @@ __device__ __forceinline__ float kvq_mag(float x) {
   const float m = fabsf(x);
   return m < INFINITY ? m : 0.f;
 }
-// x times a power of two, ready to be rounded: infinities end at the largest
+// The scale of codes on their way in: 1 / 2^(s - 127), and the largest code.  That is 448 but at s = 247, the exponent of
+// magnitudes above 448 * 2^119: there codes above 240 stand for 2^128 and more, which neither fp32 nor the
+// bf16 operands of the attention hold.
+struct KvqScale {
+  float inv, top;
+  __device__ __forceinline__ explicit KvqScale(int s) : inv(kvq_pow2(127 - s)), top(s < 247 ? 448.f : 240.f) {}
+};
+// x under the scale, ready to be rounded: infinities end at the largest
 // code, and a NaN is stored as zero (one would otherwise reach every later
 // query of its request, through a weight of zero too)
-__device__ __forceinline__ float kvq_fit(float x, float inv) {
-  const float y = fminf(fmaxf(x * inv, -448.f), 448.f);
+__device__ __forceinline__ float kvq_fit(float x, const KvqScale& sc) {
+  const float y = fminf(fmaxf(x * sc.inv, -sc.top), sc.top);
   return x == x ? y : 0.f;
 }
 // four codes, nearest with ties to even
@@ -125,7 +132,7 @@ __device__ __forceinline__ uint32_t kvq_low_bytes(int n) { return n >= 4 ? ~0u :
 
 // rows [0, n) of src to tokens off .. of a block's keys [T][D]
 template <typename E, bool VEC>
-__device__ __forceinline__ void kvq_put_keys(const E* src, size_t ld, int n, int D, int off, float inv, uint8_t* blk, int lane) {
+__device__ __forceinline__ void kvq_put_keys(const E* src, size_t ld, int n, int D, int off, const KvqScale& sc, uint8_t* blk, int lane) {
   constexpr int N = VEC ? 16 / (int)sizeof(E) : 2, U = 4;
   typedef KvqVec<E, N, VEC> V;
   const int per = D / N, step = 64 / per, c = (lane % per) * N;
@@ -139,7 +146,7 @@ __device__ __forceinline__ void kvq_put_keys(const E* src, size_t ld, int n, int
       uint8_t* p = blk + (size_t)(off + r + u * step) * D + c;
       float y[N];
 #pragma unroll
-      for (int e = 0; e < N; ++e) y[e] = kvq_fit(kvq_ld(&x[u].v[e]), inv);
+      for (int e = 0; e < N; ++e) y[e] = kvq_fit(kvq_ld(&x[u].v[e]), sc);
       if constexpr (N == 2) {
         *(uint16_t*)p = (uint16_t)kvq_code4(y[0], y[1], 0.f, 0.f);
       } else {
@@ -166,7 +173,7 @@ __device__ __forceinline__ void kvq_put16(uint8_t* row, int t0, int off, int end
 // the same for values [D][T]: a lane owns two neighbouring dims and takes 16 tokens at a time, which
 // are 16 bytes of a dim's row where the run covers them all
 template <typename E, bool VEC>
-__device__ __forceinline__ void kvq_put_values(const E* src, size_t ld, int n, int D, int T, int off, float inv, uint8_t* blk,
+__device__ __forceinline__ void kvq_put_values(const E* src, size_t ld, int n, int D, int T, int off, const KvqScale& sc, uint8_t* blk,
                                                int lane) {
   typedef KvqVec<E, 2, VEC> V;
   const int per = D / 2, d = (lane % per) * 2, groups = 64 / per;
@@ -178,7 +185,7 @@ __device__ __forceinline__ void kvq_put_values(const E* src, size_t ld, int n, i
     for (int e = 0; e < 2; ++e) {
       float y[16];
 #pragma unroll
-      for (int j = 0; j < 16; ++j) y[j] = kvq_fit(kvq_ld(&x[j].v[e]), inv);
+      for (int j = 0; j < 16; ++j) y[j] = kvq_fit(kvq_ld(&x[j].v[e]), sc);
       kvq_put16(blk + (size_t)(d + e) * T, t0, off, off + n, y);
     }
   }
@@ -219,9 +226,9 @@ struct KvqRun {
     }
   }
 };
-// The exponent for a workgroup's elements (m: a thread's largest), set; returns the factor of the codes.
+// The exponent for a workgroup's elements (m: a thread's largest), set; returns the codes' scale.
 template <typename E>
-__device__ __forceinline__ float kvq_shared_scale(const KvqRun<E>& run, int which, int T, int D, float m, uint32_t* red) {
+__device__ __forceinline__ KvqScale kvq_shared_scale(const KvqRun<E>& run, int which, int T, int D, float m, uint32_t* red) {
   m = kvq_max64(m);
   const int wave = threadIdx.x >> 6;
   if ((threadIdx.x & 63) == 0) {
@@ -238,7 +245,7 @@ __device__ __forceinline__ float kvq_shared_scale(const KvqRun<E>& run, int whic
     __syncthreads();
   }
   if (threadIdx.x == 0) *run.ep = (uint8_t)s;
-  return kvq_pow2(127 - s);
+  return KvqScale(s);
 }
 
 // a run by one wave
@@ -251,13 +258,13 @@ __device__ __forceinline__ void kvq_append_run(const KvqAppendArgs& a, int which
   const int s = max(kvq_exponent(amax), old);
   run.template rescale<64>(which, T, D, old, s, lane);
   if (lane == 0) *run.ep = (uint8_t)s;
-  const float inv = kvq_pow2(127 - s);
+  const KvqScale sc(s);
   if (which) {
-    if (vec) kvq_put_values<E, true>(run.src, run.ld, n, D, T, off, inv, run.blk, lane);
-    else kvq_put_values<E, false>(run.src, run.ld, n, D, T, off, inv, run.blk, lane);
+    if (vec) kvq_put_values<E, true>(run.src, run.ld, n, D, T, off, sc, run.blk, lane);
+    else kvq_put_values<E, false>(run.src, run.ld, n, D, T, off, sc, run.blk, lane);
   } else {
-    if (vec) kvq_put_keys<E, true>(run.src, run.ld, n, D, off, inv, run.blk, lane);
-    else kvq_put_keys<E, false>(run.src, run.ld, n, D, off, inv, run.blk, lane);
+    if (vec) kvq_put_keys<E, true>(run.src, run.ld, n, D, off, sc, run.blk, lane);
+    else kvq_put_keys<E, false>(run.src, run.ld, n, D, off, sc, run.blk, lane);
   }
 }
 
@@ -276,7 +283,7 @@ __device__ __forceinline__ void kvq_keys_shared(const KvqRun<E>& run, int T, int
   for (int u = 0; u < U; ++u)
 #pragma unroll
     for (int e = 0; e < N; ++e) m = fmaxf(m, kvq_mag(kvq_ld(&x[u].v[e])));
-  const float inv = kvq_shared_scale(run, 0, T, D, m, red);
+  const KvqScale sc = kvq_shared_scale(run, 0, T, D, m, red);
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     const int r = r0 + u * step;
@@ -284,8 +291,8 @@ __device__ __forceinline__ void kvq_keys_shared(const KvqRun<E>& run, int T, int
       KvqVec<uint32_t, N / 4, true> w;
 #pragma unroll
       for (int e = 0; e < N / 4; ++e)
-        w.v[e] = kvq_code4(kvq_fit(kvq_ld(&x[u].v[4 * e]), inv), kvq_fit(kvq_ld(&x[u].v[4 * e + 1]), inv),
-                           kvq_fit(kvq_ld(&x[u].v[4 * e + 2]), inv), kvq_fit(kvq_ld(&x[u].v[4 * e + 3]), inv));
+        w.v[e] = kvq_code4(kvq_fit(kvq_ld(&x[u].v[4 * e]), sc), kvq_fit(kvq_ld(&x[u].v[4 * e + 1]), sc),
+                           kvq_fit(kvq_ld(&x[u].v[4 * e + 2]), sc), kvq_fit(kvq_ld(&x[u].v[4 * e + 3]), sc));
       *(KvqVec<uint32_t, N / 4, true>*)(run.blk + (size_t)(run.off + r) * D + c) = w;
     }
   }
@@ -306,7 +313,7 @@ __device__ __forceinline__ void kvq_values_shared(const KvqRun<E>& run, int T, i
   for (int g = 0; g < G; ++g)
 #pragma unroll
     for (int j = 0; j < 16; ++j) m = fmaxf(m, fmaxf(kvq_mag(kvq_ld(&x[g][j].v[0])), kvq_mag(kvq_ld(&x[g][j].v[1]))));
-  const float inv = kvq_shared_scale(run, 1, T, D, m, red);
+  const KvqScale sc = kvq_shared_scale(run, 1, T, D, m, red);
 #pragma unroll
   for (int g = 0; g < G; ++g)
     if (first + g * stride < end)
@@ -314,7 +321,7 @@ __device__ __forceinline__ void kvq_values_shared(const KvqRun<E>& run, int T, i
       for (int e = 0; e < 2; ++e) {
         float y[16];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) y[j] = kvq_fit(kvq_ld(&x[g][j].v[e]), inv);
+        for (int j = 0; j < 16; ++j) y[j] = kvq_fit(kvq_ld(&x[g][j].v[e]), sc);
         kvq_put16(run.blk + (size_t)(d + e) * T, first + g * stride, off, end, y);
       }
 }

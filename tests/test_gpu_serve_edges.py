@@ -113,3 +113,48 @@ def test_attention_tiny_scales(dev, dtype, heads, kv, D, block, width, reqs, wid
     assert d < 1e-3
     worst = float((np.abs(got - want) - tol - 4 * d * top).max())
     assert worst <= 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D,rows,off", [(64, 5, 0), (128, 1, 0), (128, 16, 0), (64, 3, 8)])
+def test_append_and_read_the_largest_magnitudes(dev, dtype, D, rows, off):
+    """Magnitudes to the end of fp32 (bf16): an exponent of 247, where codes above 240 would stand for more than the type
+    holds.  Values and infinities end at 240, and the attention over them is finite."""
+    rng = np.random.default_rng(D + rows)
+    kv, block = 6, 16
+    c, arrs, plain = cache_arrays(dev, rng, 3, kv, block, D)
+    x = rng.standard_normal((rows, kv, D))
+    big = np.float32(3.3895313892515355e38)  # the largest bf16
+    x[:, 0] *= 1e37
+    x[:, 1] = np.where(rng.random((rows, D)) < 0.3, big, x[:, 1])
+    x[:, 2] = np.where(rng.random((rows, D)) < 0.3, -big, np.clip(x[:, 2] * 2.5e37, -1e38, 1e38))
+    x[:, 3] = np.where(rng.random((rows, D)) < 0.3, np.inf, np.clip(x[:, 3] * 2e38, -big, big))
+    x[:, 4] = np.resize(np.array([2.0 ** 127 * 1.75, 2.0 ** 127 * 1.6, -2.0 ** 127, 3e38]), (rows, D))
+    x[:, 5] = np.resize(np.array([2.0 ** 127 * 1.765625, -np.inf, 2.0 ** 127 * 1.9375, 2.0 ** 127 * 1.875, 2.0 ** 127 * 1.8125]), (rows, D))
+    x[0, 1:3, 0] = big
+    x = x.astype(np.float32)
+    if dtype == "f32":
+        x[0, 1, 1] = np.finfo(np.float32).max
+    raw, val = typed(x, dtype)
+    slots = (block + off + np.arange(rows)).astype(np.int32)
+    dk, dv = dev(raw), dev(raw[:, ::-1].copy())
+    ssd.ssd_kvq_append(c, ssd.ssd_kvq_append_params(code(dtype), rows, kv * D, kv * D), dev(slots).ptr, dk.ptr, dv.ptr)
+    k, v, ke, ve = [a.numpy() for a in arrs]
+    for h in range(kv):
+        for codes, exps, head, old in ((S.E4M3[k[1, h, off:off + rows]], ke, h, plain.ke), (S.E4M3[v[1, h]].T[off:off + rows], ve, kv - 1 - h, plain.ve)):
+            y = val[:, head]
+            s = max(S.exponent(np.abs(y[np.isfinite(y)]).max()), old[1, h] if off else 1)
+            assert exps[1, h] == s
+            top = 240.0 if s == 247 else 448.0
+            assert np.array_equal(codes, S.e4m3_round(np.clip(y * 2.0 ** (127 - s), -top, top)))
+    stands = np.abs(S.E4M3[k[1]][:, off:off + rows] * np.exp2(ke[1] - 127.0)[:, None, None]).max()
+    assert (ke[1] == 247).any() and stands <= big
+    if off:
+        return
+    # The attention that sees the first token returns its values.  (Sums are fp32, and 2 * 240 * 2^120 is past it: a row that
+    # sees several such values has no finite sum.)
+    q = typed(np.zeros((1, kv, D)), dtype)[0]
+    got = attend(dev, c, dtype, q, [0, 1], [1], np.array([[1]]), 1.0)
+    want = (S.E4M3[v[1]][:, :, 0] * np.exp2(ve[1] - 127.0)[:, None])[None]
+    worst = float((np.abs(got - want) - np.abs(want) * (2.0 ** -8 + 2.0 ** -11 + 32 * 2.0 ** -24)).max())
+    assert worst <= 0
