@@ -30,8 +30,9 @@ struct ArrayCheck {
     }
   }
   void need(const char* name, const void* p, size_t bytes, size_t align) {
-    if (bad || !bytes) return;
     const uintptr_t at = (uintptr_t)p;
+    if (bytes > (size_t)PTRDIFF_MAX) bad = name;  // (on any machine: no array is that long)
+    if (bad || !bytes) return;
     if (!p || (at & (align - 1))) {
       bad = name;
       return;
@@ -63,7 +64,14 @@ struct ArrayCheck {
   }
 };
 
-size_t span(size_t rows, size_t ld, size_t cols, size_t es) { return rows ? ((rows - 1) * ld + cols) * es : 0; }
+// bytes of rows of cols elements, ld apart; where they pass 64 bits, more than any array has
+size_t span(size_t rows, size_t ld, size_t cols, size_t es) {
+  size_t n = 0;
+  if (!rows) return 0;
+  return __builtin_mul_overflow(rows - 1, ld, &n) || __builtin_add_overflow(n, cols, &n) || __builtin_mul_overflow(n, es, &n)
+             ? SIZE_MAX
+             : n;
+}
 
 ssd_status launched(const char* what) {
   const hipError_t e = hipGetLastError();
