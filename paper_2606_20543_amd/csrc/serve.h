@@ -14,10 +14,11 @@ namespace ssd {
 // is pool[sum of the lacks before b].  A workgroup owns SLOT_SEQS requests and
 // sums the lengths of all requests before them itself (a few loads a thread),
 // so one launch does it with no hand-off between workgroups; several share the rows
-// of the same requests where there are many.  Bound by its
+// of the same requests where there are many.  (More than some thousand requests take four launches.)  Bound by its
 // launch and three dependent round trips (lengths, table or pool entry, store): 64
 // requests of one new token 7.6 us a call (5.3 the kernel), 2048 of up to 64 7.7.
 constexpr int SLOT_T = 256, SLOT_SEQS = 8;
+constexpr int SLOT_ALONE = 8192;  // most requests of the single launch
 
 __device__ __forceinline__ long long wave_sum_ll(long long v) {
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
@@ -111,7 +112,161 @@ __global__ __launch_bounds__(SLOT_T) void slots_kernel(SlotArgs a) {
     a.slots[r] = a.positions[r] = -1;
 }
 
+// Many requests: sums of chunks of them, the sums before each chunk, then the requests and at last the rows, each by a
+// launch of its own.  A chunk's two numbers (rows and lacking blocks, of it and then before it) wait between the
+// launches in its first four entries of lens, which only its own workgroup writes.
+constexpr int SLOT_CHUNK = 256, SLOT_SCAN_T = 1024;
+
+struct SlotSums {
+  long long rows, lack;
+};
+__device__ __forceinline__ SlotSums slot_sums_load(const int* p) {
+  const unsigned a = p[0], b = p[1], c = p[2], d = p[3];
+  return SlotSums{(long long)((unsigned long long)b << 32 | a), (long long)((unsigned long long)d << 32 | c)};
+}
+__device__ __forceinline__ void slot_sums_store(int* p, const SlotSums& s) {
+  p[0] = (int)s.rows, p[1] = (int)(s.rows >> 32), p[2] = (int)s.lack, p[3] = (int)(s.lack >> 32);
+}
+// sums of the threads before this one, and of all; red: N / 64 entries
+template <int N>
+__device__ __forceinline__ SlotSums slot_scan(SlotSums x, SlotSums* red, SlotSums& all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  SlotSums s = x;
+  for (int o = 1; o < 64; o <<= 1) {
+    const long long r = __shfl_up(s.rows, o), l = __shfl_up(s.lack, o);
+    if (lane >= o) s.rows += r, s.lack += l;
+  }
+  if (lane == 63) red[wave] = s;
+  __syncthreads();
+  SlotSums before{s.rows - x.rows, s.lack - x.lack};
+  all = SlotSums{0, 0};
+  for (int w = 0; w < N / 64; ++w) {
+    if (w < wave) before.rows += red[w].rows, before.lack += red[w].lack;
+    all.rows += red[w].rows, all.lack += red[w].lack;
+  }
+  return before;
+}
+// a chunk's requests (the last takes the rest: every chunk has SLOT_CHUNK at least)
+__device__ __forceinline__ int slot_chunk_end(const SlotArgs& a, int chunk, int chunks) {
+  return chunk == chunks - 1 ? a.B : (chunk + 1) * SLOT_CHUNK;
+}
+
+__global__ __launch_bounds__(SLOT_T) void slots_sums_kernel(SlotArgs a) {
+  __shared__ SlotSums red[SLOT_T / 64];
+  const int b0 = blockIdx.x * SLOT_CHUNK, end = slot_chunk_end(a, blockIdx.x, gridDim.x), sh = __builtin_ctz(a.T);
+  SlotSums s{0, 0}, all;
+  for (int b = b0 + threadIdx.x; b < end; b += SLOT_T) {
+    const long long h = max(a.held[b], 0), n = max(a.fresh[b], 0);
+    s.rows += n;
+    s.lack += slot_blocks(h + n, a.T, sh, a.width) - slot_blocks(h, a.T, sh, a.width);
+  }
+  slot_scan<SLOT_T>(s, red, all);
+  if (threadIdx.x == 0) slot_sums_store(a.lens + b0, all);
+}
+
+__global__ __launch_bounds__(SLOT_SCAN_T) void slots_scan_kernel(SlotArgs a, int chunks) {
+  __shared__ SlotSums red[SLOT_SCAN_T / 64];
+  const int per = (chunks + SLOT_SCAN_T - 1) / SLOT_SCAN_T, c0 = threadIdx.x * per, end = min(c0 + per, chunks);
+  SlotSums s{0, 0}, all;
+  for (int c = c0; c < end; ++c) {
+    const SlotSums x = slot_sums_load(a.lens + (size_t)c * SLOT_CHUNK);
+    s.rows += x.rows, s.lack += x.lack;
+  }
+  SlotSums before = slot_scan<SLOT_SCAN_T>(s, red, all);
+  for (int c = c0; c < end; ++c) {
+    int* p = a.lens + (size_t)c * SLOT_CHUNK;
+    const SlotSums x = slot_sums_load(p);
+    slot_sums_store(p, before);
+    before.rows += x.rows, before.lack += x.lack;
+  }
+  if (threadIdx.x == 0) {
+    a.cu[0] = 0;
+    a.used[0] = (int)min(all.lack, (long long)INT_MAX);
+  }
+}
+
+__global__ __launch_bounds__(SLOT_T) void slots_requests_kernel(SlotArgs a) {
+  constexpr int MOST = 2 * SLOT_CHUNK, PER = MOST / SLOT_T;  // requests of a chunk and of a thread
+  __shared__ SlotSums red[SLOT_T / 64];
+  __shared__ long long s_start[MOST + 1];
+  __shared__ int s_have[MOST];
+  const int tid = threadIdx.x, b0 = blockIdx.x * SLOT_CHUNK, nb = slot_chunk_end(a, blockIdx.x, gridDim.x) - b0;
+  const int sh = __builtin_ctz(a.T), W = a.width;
+  const SlotSums at = slot_sums_load(a.lens + b0);
+  long long held[PER], fresh[PER];
+  int have[PER], lack[PER];
+  SlotSums s{0, 0}, all;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int b = tid * PER + i;
+    held[i] = b < nb ? max(a.held[b0 + b], 0) : 0;
+    fresh[i] = b < nb ? max(a.fresh[b0 + b], 0) : 0;
+    have[i] = slot_blocks(held[i], a.T, sh, W);
+    lack[i] = slot_blocks(held[i] + fresh[i], a.T, sh, W) - have[i];
+    s.rows += fresh[i], s.lack += lack[i];
+  }
+  SlotSums before = slot_scan<SLOT_T>(s, red, all);  // (a barrier: everyone has read the chunk's sums)
+  before.rows += at.rows, before.lack += at.lack;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int b = tid * PER + i;
+    if (b < nb) {
+      s_start[b] = before.lack;
+      s_have[b] = have[i];
+      before.rows += fresh[i], before.lack += lack[i];
+      a.cu[b0 + b + 1] = (int)min(before.rows, (long long)INT_MAX);
+      a.lens[b0 + b] = (int)min(held[i] + fresh[i], (long long)INT_MAX);
+      if (b == nb - 1) s_start[nb] = before.lack;
+    }
+  }
+  __syncthreads();
+  // entries of the blocks taken here (an empty pool leaves -1)
+  for (long long e = s_start[0] + tid; e < s_start[nb]; e += SLOT_T) {
+    int lo = 0, hi = nb;  // the last request that starts at e or before
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (s_start[mid] <= e) lo = mid;
+      else hi = mid;
+    }
+    a.table[(size_t)(b0 + lo) * W + s_have[lo] + (e - s_start[lo])] = e < a.n_pool ? a.pool[e] : -1;
+  }
+}
+
+__global__ __launch_bounds__(SLOT_T) void slots_rows_kernel(SlotArgs a) {
+  const int sh = __builtin_ctz(a.T);
+  for (long long r = (long long)blockIdx.x * SLOT_T + threadIdx.x; r < a.n_rows; r += (long long)gridDim.x * SLOT_T) {
+    int slot = -1, pos = -1, lo = 0, hi = a.B;  // the last request whose rows begin at r or before
+    if (r < a.cu[a.B]) {
+      while (hi - lo > 1) {
+        const int mid = lo + (hi - lo) / 2;
+        if (a.cu[mid] <= r) lo = mid;
+        else hi = mid;
+      }
+      const long long p = (long long)max(a.held[lo], 0) + (r - a.cu[lo]), j = p >> sh;
+      if (j < a.width) {
+        const int page = a.table[(size_t)lo * a.width + j];
+        const long long at = (long long)page * a.T + (p & (a.T - 1));
+        if (page >= 0 && at <= INT_MAX) slot = (int)at;
+      }
+      pos = (int)min(p, (long long)INT_MAX);
+    }
+    a.slots[r] = slot;
+    a.positions[r] = pos;
+  }
+}
+
 void kvq_slots(const SlotArgs& a, hipStream_t st) {
+  // Each workgroup of the single launch reads all lengths, a square of the requests in all.  us a call of single tokens, one
+  // launch and four: 4096 requests 9.6 and 14.5, 8192 14.0 and 14.5, 16384 29 and 14.7, 131072 3510 and 18.6, 2^20 53 by four.
+  if (a.B > SLOT_ALONE) {
+    const int chunks = a.B / SLOT_CHUNK;
+    hipLaunchKernelGGL(slots_sums_kernel, dim3(chunks), dim3(SLOT_T), 0, st, a);
+    hipLaunchKernelGGL(slots_scan_kernel, dim3(1), dim3(SLOT_SCAN_T), 0, st, a, chunks);
+    hipLaunchKernelGGL(slots_requests_kernel, dim3(chunks), dim3(SLOT_T), 0, st, a);
+    if (a.n_rows)
+      hipLaunchKernelGGL(slots_rows_kernel, dim3((unsigned)std::min(4096ll, ((long long)a.n_rows + SLOT_T - 1) / SLOT_T)), dim3(SLOT_T), 0, st, a);
+    return;
+  }
   // Workgroups for the same requests' rows: one for each 1024 of the rows that a group gets on average (a
   // prompt of 65536: 88 us with one, 4.6 with 64), and with many rows up to four for a group that gets more (one
   // such prompt among 2047 single tokens: 91 us with one, 31 with four, 26 with eight, which take

@@ -158,3 +158,80 @@ def test_append_and_read_the_largest_magnitudes(dev, dtype, D, rows, off):
     want = (S.E4M3[v[1]][:, :, 0] * np.exp2(ve[1] - 127.0)[:, None])[None]
     worst = float((np.abs(got - want) - np.abs(want) * (2.0 ** -8 + 2.0 ** -11 + 32 * 2.0 ** -24)).max())
     assert worst <= 0
+
+
+def slots_of(held, fresh, pool, table, block, n_rows):
+    """tests/serve_util.py's slots without loops over requests; lengths and positions end at the largest int32."""
+    top = 2 ** 31 - 1
+    B, W = table.shape
+    held, fresh = np.maximum(held.astype(np.int64), 0), np.maximum(fresh.astype(np.int64), 0)
+    lens = held + fresh
+    have, want = np.minimum(-(-held // block), W), np.minimum(-(-lens // block), W)
+    take = want - have
+    start, cu = np.cumsum(take) - take, np.concatenate([[0], np.cumsum(fresh)])
+    total = int(take.sum())
+    served = np.concatenate([pool.astype(np.int64), np.full(max(0, total - len(pool)), -1)])
+    table = table.copy()
+    b = np.repeat(np.arange(B), take)
+    table[b, have[b] + np.arange(total) - start[b]] = served[:total]
+    n = min(n_rows, int(cu[-1]))
+    slots, positions = np.full(n_rows, -1, np.int64), np.full(n_rows, -1, np.int64)
+    b = np.searchsorted(cu[1:], np.arange(n), side="right")
+    p = held[b] + np.arange(n) - cu[b]
+    page = np.where(p // block < W, table[b, np.minimum(p // block, W - 1)], -1)
+    positions[:n] = np.minimum(p, top)
+    slots[:n] = np.where(page >= 0, page.astype(np.int64) * block + p % block, -1)
+    return dict(table=table, lens=np.minimum(lens, top), cu=np.minimum(cu, top), slots=slots, positions=positions,
+                used=np.array([total]))
+
+
+MANY_REQUESTS = [  # B, block, width, held, fresh, short of blocks, padded rows, rows cut
+    (2049, 16, 6, 90, 2, 0, 5, 0), (4097, 32, 3, 60, 5, 40, 0, 17), (8192, 16, 5, 90, 2, 0, 5, 0),
+                 (8193, 16, 5, 90, 2, 30, 0, 5), (10000, 128, 2, 200, 90, 0, 3000, 0), (33333, 64, 4, 300, 1, 0, 0, 0),
+    (100000, 16, 5, 70, 3, 1000, 9, 0), (262144, 32, 2, 30, 1, 0, 0, 100), (2 ** 20 - 1, 16, 3, 40, 1, 0, 1, 0), (2 ** 20, 16, 2, 30, 2, 9, 0, 0)]
+
+
+@pytest.mark.parametrize("B,block,width,held,fresh,short,pad,cut", MANY_REQUESTS)
+def test_slots_of_many_requests(dev, B, block, width, held, fresh, short, pad, cut):
+    rng = np.random.default_rng(B + block)
+    h, f, pool, table, n = slot_case(rng, B, block, width, held, fresh, short, pad, cut)
+    h[3], f[4] = -5, -2  # count as 0
+    table[3] = np.maximum(table[3], 0)
+    f[B // 2] = 900  # a prompt among them, past the table's width
+    n += 900
+    if B < 5000:
+        want = slots_of(h, f, pool, table, block, n)
+        for name, w in S.slots(h, f, pool, table, block, n).items():
+            assert np.array_equal(want[name], w), name
+    h[rng.integers(0, B, 9)] = 2 ** 31 - 1
+    want = slots_of(h, f, pool, table, block, n)
+    p = ssd.ssd_kvq_slot_params(B, block, width, len(pool), n)
+    ins = [dev(x) for x in (h, f, pool)]
+    t = dev(table)
+    outs = [dev(np.full(max(1, x), 99, np.int32)) for x in (B, B + 1, n, n, 1)]
+    for _ in range(2):  # again: the same
+        ssd.ssd_kvq_slots(p, *[x.ptr for x in ins], t.ptr, *[x.ptr for x in outs])
+        for name, a in zip(("table", "lens", "cu", "slots", "positions", "used"), [t] + outs):
+            w = want[name].reshape(-1)
+            assert np.array_equal(a.numpy().reshape(-1)[:w.size], w), name
+
+
+def test_slots_time_grows_with_the_requests(dev):
+    """2^20 single tokens: a few passes over some 20 MB.  Summing all lengths in every workgroup took 4 TB of reads."""
+    hip = G.DeviceArray.hip()
+    B = 2 ** 20
+    h, f = dev(np.full(B, 15, np.int32)), dev(np.full(B, 2, np.int32))
+    pool, table = dev(np.arange(B, dtype=np.int32)), dev(np.zeros((B, 2), np.int32))
+    outs = [dev(np.zeros(x, np.int32)) for x in (B, B + 1, 2 * B, 2 * B, 1)]
+    p = ssd.ssd_kvq_slot_params(B, 16, 2, B, 2 * B)
+    start, stop = ctypes.c_void_p(), ctypes.c_void_p()
+    assert hip.hipEventCreate(ctypes.byref(start)) == 0 and hip.hipEventCreate(ctypes.byref(stop)) == 0
+    ms = ctypes.c_float()
+    for _ in range(2):
+        assert hip.hipEventRecord(start, None) == 0
+        ssd.ssd_kvq_slots(p, h.ptr, f.ptr, pool.ptr, table.ptr, *[x.ptr for x in outs])
+        assert hip.hipEventRecord(stop, None) == 0 and hip.hipEventSynchronize(stop) == 0
+        assert hip.hipEventElapsedTime(ctypes.byref(ms), start, stop) == 0
+    hip.hipEventDestroy(start), hip.hipEventDestroy(stop)
+    assert outs[4].numpy()[0] == B
+    assert ms.value < 20.0  # (some 0.1)
