@@ -383,7 +383,8 @@ void rope_axes_table(const RopeTableArgs& a, hipStream_t st) {
 
 // ---------------- a session's cache as rows ----------------
 // One thread copies eight dims of one position and head: 16 bytes of a key tile, and the value
-// tiles' elements one by one.
+// tiles' elements one by one.  VEC: the outputs start on 16 bytes, else they are written by elements.
+template <bool VEC>
 __global__ __launch_bounds__(256) void read_kv_bf16_kernel(int B, int n, int Hkv, int D, int Lmax, const uint16_t* kc,
                                                            const uint16_t* vc, uint16_t* k, uint16_t* v) {
   const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
@@ -391,11 +392,17 @@ __global__ __launch_bounds__(256) void read_kv_bf16_kernel(int B, int n, int Hkv
   if (i >= (size_t)B * n * Hkv * per) return;
   const int c = (int)(i % per), h = (int)(i / per % Hkv), p = (int)(i / ((size_t)per * Hkv) % n);
   const size_t b = i / ((size_t)per * Hkv * n), base = (b * Hkv + h) * (size_t)Lmax * D;
-  *(uint4*)(k + i * 8) = *(const uint4*)(kc + base + tile16x32_index(p, c * 8, D));
-  uint16_t x[8];
+  RopeVec<uint16_t, 8> x, y;
+  x = *(const RopeVec<uint16_t, 8>*)(kc + base + tile16x32_index(p, c * 8, D));
 #pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = vc[base + vtile_index(c * 8 + e, p, Lmax)];
-  *(uint4*)(v + i * 8) = *(const uint4*)x;
+  for (int e = 0; e < 8; ++e) y.v[e] = vc[base + vtile_index(c * 8 + e, p, Lmax)];
+  if constexpr (VEC) {
+    *(RopeVec<uint16_t, 8>*)(k + i * 8) = x;
+    *(RopeVec<uint16_t, 8>*)(v + i * 8) = y;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) k[i * 8 + e] = x.v[e], v[i * 8 + e] = y.v[e];
+  }
 }
 __global__ __launch_bounds__(256) void read_kv_f32_kernel(int B, int n, int Hkv, int D, int Lmax, const float* kc, const float* vc,
                                                           float* k, float* v) {
@@ -409,9 +416,10 @@ __global__ __launch_bounds__(256) void read_kv_f32_kernel(int B, int n, int Hkv,
 
 void read_kv(const Dims& dm, int B, int n, int Lmax, const void* kc, const void* vc, void* k, void* v, hipStream_t st) {
   const size_t all = (size_t)B * n * dm.Hkv * dm.D;
+  const bool vec = (((uintptr_t)k | (uintptr_t)v) & 15) == 0;
   if (dm.bf16)
-    hipLaunchKernelGGL(read_kv_bf16_kernel, dim3((unsigned)((all / 8 + 255) / 256)), dim3(256), 0, st, B, n, dm.Hkv, dm.D, Lmax,
-                       (const uint16_t*)kc, (const uint16_t*)vc, (uint16_t*)k, (uint16_t*)v);
+    hipLaunchKernelGGL(vec ? read_kv_bf16_kernel<true> : read_kv_bf16_kernel<false>, dim3((unsigned)((all / 8 + 255) / 256)), dim3(256),
+                       0, st, B, n, dm.Hkv, dm.D, Lmax, (const uint16_t*)kc, (const uint16_t*)vc, (uint16_t*)k, (uint16_t*)v);
   else
     hipLaunchKernelGGL(read_kv_f32_kernel, dim3((unsigned)((all + 255) / 256)), dim3(256), 0, st, B, n, dm.Hkv, dm.D, Lmax,
                        (const float*)kc, (const float*)vc, (float*)k, (float*)v);

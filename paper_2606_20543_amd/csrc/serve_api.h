@@ -398,8 +398,8 @@ ssd_status ssd_session_read_kv(ssd_session* s, int32_t layer, int32_t n, void* k
     if (n < 1 || n > s->f[b]) return fail(SSD_E_INVAL, "n = %d outside [1, frontier = %d]", n, s->f[b]);
   const size_t es = esize(s->dm), bytes = (size_t)s->B * n * s->dm.Hkv * s->dm.D * es;
   ArrayCheck ck(s->stream);
-  ck.need("k_out", k_out, bytes, 16);
-  ck.need("v_out", v_out, bytes, 16);
+  ck.need("k_out", k_out, bytes, es);
+  ck.need("v_out", v_out, bytes, es);
   if (ck.bad) return ck.status();
   const size_t at = (size_t)layer * s->kv_layer_elems * es;
   read_kv(s->dm, s->B, n, s->Lmax, (const char*)s->kc + at, (const char*)s->vc + at, k_out, v_out, s->stream);

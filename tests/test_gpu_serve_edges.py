@@ -235,3 +235,36 @@ def test_slots_time_grows_with_the_requests(dev):
     hip.hipEventDestroy(start), hip.hipEventDestroy(stop)
     assert outs[4].numpy()[0] == B
     assert ms.value < 20.0  # (some 0.1)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_session_rows_at_any_element(dtype):
+    """A layer's cached rows into arrays that start on an element, not on 16 bytes: the rows an aligned array gets, and
+    nothing around them."""
+    shape = synth.TINY if dtype == "f32" else dataclasses.replace(synth.M1B, n_layers=2)
+    pair = G.Pair(shape, oracle=False)
+    B, P = 3, 19
+    sess = ssd.ssd_prefill(pair.model, B, P, synth.prompt(shape, B, P).astype(np.int32), P + 4, 4)
+    raw = np.uint16 if dtype == "bf16" else np.float32
+    n = B * P * shape.n_kv_heads * shape.head_dim
+    aligned = [G.DeviceArray(np.zeros(n, raw)) for _ in range(2)]
+    odd = [G.DeviceArray(np.full(n + 16, 3, raw)) for _ in range(2)]
+    try:
+        ssd.ssd_session_read_kv(sess, 1, P, aligned[0].ptr, aligned[1].ptr)
+        for ka, va in ((1, 3), (0, 5), (7, 8)):
+            for a in odd:
+                upload(a, np.full(n + 16, 3, raw))
+            es = np.dtype(raw).itemsize
+            ssd.ssd_session_read_kv(sess, 1, P, odd[0].ptr + ka * es, odd[1].ptr + va * es)
+            for a, want, at in zip(odd, aligned, (ka, va)):
+                got = a.numpy()
+                assert np.array_equal(got[at:at + n], want.numpy())
+                assert (got[:at] == 3).all() and (got[at + n:] == 3).all()
+        with pytest.raises(ssd.SSDError) as e:  # inside an element
+            ssd.ssd_session_read_kv(sess, 1, P, odd[0].ptr + 1, odd[1].ptr)
+        assert e.value.status == ssd.SSD_E_INVAL
+    finally:
+        for a in aligned + odd:
+            a.free()
+        ssd.ssd_free_session(sess)
+        pair.close()
