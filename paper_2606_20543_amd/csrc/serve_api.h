@@ -17,6 +17,7 @@ struct ArrayCheck {
   } seen[4];
   explicit ArrayCheck(void* stream) {
     hipDevice_t sd = -1;
+    (void)hipGetLastError();  // what an earlier call of the thread left is not this one's (launched() asks for its own)
     if (hipGetDevice(&dev) != hipSuccess) {
       (void)hipGetLastError();
       bad = "no GPU";
@@ -383,6 +384,7 @@ ssd_status ssd_session_set_axes(ssd_session* s, int32_t n_axes, const int32_t* s
   a.half = s->dm.D / 2;
   a.theta = (double)s->dm.theta;
   a.tab = s->rope + (size_t)s->P * a.half;
+  (void)hipGetLastError();  // (as in ArrayCheck)
   rope_axes_table(a, s->stream);
   const ssd_status ls = launched("ssd_session_set_axes");
   if (ls != SSD_OK) s->poisoned = true;

@@ -268,3 +268,37 @@ def test_session_rows_at_any_element(dtype):
             a.free()
         ssd.ssd_free_session(sess)
         pair.close()
+
+
+def test_an_error_of_an_earlier_call_is_not_this_ones(dev):
+    """An error that other code of the thread left behind (a copy that the runtime refused) does not fail a call that works."""
+    hip = G.DeviceArray.hip()
+    rng = np.random.default_rng(4)
+    c, arrs, plain = cache_arrays(dev, rng, 3, 2, 16, 64)
+    rows, ints, out = dev(np.ones((4, 128), np.float32)), dev(np.arange(16, dtype=np.int32)), dev(np.zeros((4, 128), np.float32))
+    i32 = [dev(np.zeros(16, np.int32)) for _ in range(6)]
+    rope = ssd.ssd_rope_params(2, 2, 64, ssd.SSD_F32, 1, (32,), 128, 128, 128, 128, 1e4)
+    attn = ssd.ssd_kvq_attn_params(ssd.SSD_F32, 1, 4, 2, 1, 16, 1, 128, 128, 0.125, 0)
+    calls = [lambda: ssd.ssd_kvq_slots(ssd.ssd_kvq_slot_params(2, 16, 2, 4, 4), ints.ptr, ints.ptr, ints.ptr, *[x.ptr for x in i32]),
+             lambda: ssd.ssd_rope_axes(rope, 4, rows.ptr, rows.ptr, ints.ptr, out.ptr, arrs[0].ptr),
+             lambda: ssd.ssd_kvq_append(c, ssd.ssd_kvq_append_params(ssd.SSD_F32, 4, 128, 128), ints.ptr, rows.ptr, rows.ptr),
+             lambda: ssd.ssd_kvq_attention(c, attn, rows.ptr, ints.ptr, ints.ptr, i32[0].ptr, out.ptr),
+             lambda: ssd.ssd_sample_logits(ssd.ssd_sample_params(vocab=128, ld=128, temperature=1.0, top_p=1.0), 4, rows.ptr, rows.ptr, ints.ptr)]
+    shape = synth.TINY
+    pair = G.Pair(shape, oracle=False)
+    sess = ssd.ssd_prefill(pair.model, 1, 5, synth.prompt(shape, 1, 5).astype(np.int32), 9, 4)
+    axes = dev(np.zeros((2, 4), np.int32))
+    row = dev(np.zeros((2, 5 * shape.n_kv_heads * shape.head_dim), np.float32))
+    half = shape.head_dim // 4
+    calls += [lambda: ssd.ssd_session_set_axes(sess, (half, half), axes.ptr),
+              lambda: ssd.ssd_session_sample(sess, ssd.ssd_sample_params(temperature=1.0, top_p=1.0), rows.ptr, ints.ptr),
+              lambda: ssd.ssd_session_read_kv(sess, 0, 5, row.ptr, row.ptr + row.nbytes // 2)]
+    try:
+        for call in calls:
+            assert hip.hipMemcpy(None, None, 16, 1) != 0
+            call()
+        assert hip.hipDeviceSynchronize() == 0
+    finally:
+        hip.hipGetLastError()
+        ssd.ssd_free_session(sess)
+        pair.close()
