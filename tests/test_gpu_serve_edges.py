@@ -116,6 +116,30 @@ def test_attention_tiny_scales(dev, dtype, heads, kv, D, block, width, reqs, wid
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("cu,max_q", [([-2, 2, 6], 4), ([0, 2, 10 ** 6], 4), ([5, 3, 200], 4), ([2 ** 31 - 1, -2 ** 31, 4], 4),
+                                      ([0, 9, 9], 4), ([9, 12, 9], 4), ([7, 11, 20], 20), ([-5, -1, 3], 20), ([2, 2, 2], 1)])
+def test_attention_row_offsets_anywhere(dev, dtype, cu, max_q):
+    """Rows that cu puts outside the array are skipped, rows past max_q are not computed, and no other row is written."""
+    rng = np.random.default_rng(10)
+    heads, kv, D, block, rows = 4, 2, 64, 16, 9
+    c, arrs, plain = cache_arrays(dev, rng, 5, kv, block, D)
+    table, lens = np.array([[3, 1], [0, 4]], np.int32), [30, 25]
+    q, val = typed(rng.standard_normal((rows, heads, D)), dtype)
+    got = attend(dev, c, dtype, q, cu, lens, table, 0.125, max_q=max_q)
+    want, tol = np.full(q.shape, np.nan), np.zeros(q.shape)
+    for b in range(2):
+        n = cu[b + 1] - cu[b]
+        if not 0 < n < 2 ** 24:  # (2^32: all of its first rows lie before the array)
+            continue
+        w, t = S.attention(plain, val, [cu[b], cu[b + 1]], lens[b:b + 1], table[b:b + 1], 0.125, dtype == "bf16")
+        for r in range(max(0, cu[b]), min(rows, cu[b + 1], cu[b] + max_q)):
+            want[r], tol[r] = w[r], t[r]
+    none = np.isnan(want)
+    assert (got[none] == 77.0).all()
+    assert (np.abs(got - want) <= tol)[~none].all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("D,rows,off", [(64, 5, 0), (128, 1, 0), (128, 16, 0), (64, 3, 8)])
 def test_append_and_read_the_largest_magnitudes(dev, dtype, D, rows, off):
     """Magnitudes to the end of fp32 (bf16): an exponent of 247, where codes above 240 would stand for more than the type
