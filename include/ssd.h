@@ -432,6 +432,9 @@ ssd_status ssd_decode_image_heads(ssd_model* model, const ssd_schedule* sched, i
  *  - What the host cannot see (lengths, tables, slots) is bounds-checked by the
  *    kernels: an entry that names no block or no row is skipped as each call says.
  *  - SSD_E_DEVICE here poisons nothing: the arrays may hold part of a result.
+ *  - Heads (n_heads, n_kv_heads) are at most 65535.
+ * The session calls at the end (ssd_session_sample, _set_axes, _read_kv) take their arrays as these do, on the
+ * session's stream; what ssd_session_set_axes does besides is said there.
  */
 
 /*
@@ -546,7 +549,8 @@ ssd_status ssd_kvq_append(const ssd_kvq_cache* cache, const ssd_kvq_append_param
  *     out = softmax(scale * q k^T) v,   head h reads KV head h / (n_heads / n_kv_heads)
  * q [n_rows][n_heads][head_dim] with row length ld_q (elements), out likewise with ld_out
  * (may be q where ld_out = ld_q), dtype SSD_F32 or SSD_BF16; statistics and sums are
- * fp32, the result is rounded once.  Rows that cu names outside [0, n_rows) are skipped.
+ * fp32, the result is rounded once.  Bf16 calls also round every weight, times the scale of its value's block, to
+ * fp16: 11 bits, and in steps of 2^-30 of the largest such product in the row.  Rows that cu names outside [0, n_rows) are skipped.
  * table [n_seqs][table_width]: entries outside [0, n_blocks) hide their positions; so
  * do positions past the table's width.  A row that sees no position gets zeros.
  * Rows of out that belong to no request stay as they were.
@@ -627,8 +631,10 @@ ssd_status ssd_session_sample(ssd_session* sess, const ssd_sample_params* params
  * P + i (the same for all sequences: row and column of a grid, say), host or
  * device.  The prompt keeps its raster positions, which are equal on all axes.
  * Before anything was committed behind the prompt (SSD_E_STATE otherwise; a second
- * call replaces the first).  Errors: SSD_E_INVAL for NULL arguments or
- * bad sections; SSD_E_OOM.
+ * call replaces the first).  The first call of a session allocates (16 bytes a position), and positions
+ * in host memory are read before the call returns, which waits for the session's stream: not for a
+ * stream that is being captured.  Errors: SSD_E_INVAL for NULL arguments or bad sections; SSD_E_OOM;
+ * SSD_E_DEVICE (the session is unusable where its table could not be written).
  */
 ssd_status ssd_session_set_axes(ssd_session* sess, int32_t n_axes, const int32_t* section, const int32_t* positions);
 

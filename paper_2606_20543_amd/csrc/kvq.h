@@ -63,8 +63,8 @@ __device__ __forceinline__ void kvq_value4(uint32_t codes, float (&v)[4]) {
 // the scale grew, then the run is stored.
 //
 // Nothing is computed to speak of: the bytes bound it (8 heads of 128, 16 prompts of up to 2048
-// rows after one: 134 MB, 26 us at the rate of a large copy; 41 us a call, 36 of them the
-// kernel), and, for single tokens, the launch (7.4 us a call).  Where a window of rows starts one or
+// rows after one: 134 MB, 26 us at the rate of a large copy; 41 us a call, 38 of them the
+// kernel), and, for single tokens, the launch (8.1 us a call, 6.5 the kernel).  Where a window of rows starts one or
 // two runs, a workgroup takes them together and holds the elements between the maximum and the
 // codes, so the rows are read once; where it starts more (short runs), a wave takes each and
 // reads it a second time, from the caches (every run by a wave of its own: 47 us for the prompts).
@@ -408,7 +408,8 @@ void kvq_append(KvqAppendArgs a, hipStream_t st) {
 // the weights take the value scale along, p' = 2^(t - m + e - R), e the value exponent of the
 // key's block and R a running bound of t - m + e, so that the codes themselves, exact in fp16,
 // are the other operand whatever the scales of different blocks are; p' is rounded to fp16,
-// 11 bits where the output has 8.  p' is formed alone, a lane's 16 of a step share e, so l takes
+// 11 bits where the output has 8 (8 x 64 rows are 0.00167 of their norm off the result in 64 bits, which rounded to bf16
+// is 0.00166 off).  p' is formed alone, a lane's 16 of a step share e, so l takes
 // their sum times 2^(R - e).  m and R follow their maxima lazily: only where a lane
 // finds one grown by more than 2^8 are the maxima of all lanes taken and the sums rescaled.
 //
@@ -778,8 +779,8 @@ struct KvqGeom {
 // and one share of its keys; wave w takes every fourth step, a step's codes in
 // registers while the next step's are on their way, and the four meet in LDS.
 // For few rows, where the cache's bytes bound it: single tokens of 64 requests of up to 16384, 8 heads
-// of 128, 1296 MB in 240 us, 5.4 TB/s (a large copy reads and writes 5.1); a single request of 412
-// is latency (7.5 us a call).
+// of 128, 1296 MB in 243 us, 5.3 TB/s (a large copy reads and writes 5.1 to 5.2); a single request of 412
+// is latency (7.7 us a call).
 template <typename E, int D, int QT>
 __global__ __launch_bounds__(256) void kvq_attn_keys_kernel(KvqAttnArgs a) {
   constexpr int ROWS = 16 * QT, RS = D + 4;
@@ -885,10 +886,11 @@ __global__ __launch_bounds__(256) void kvq_attn_keys_kernel(KvqAttnArgs a) {
 // of them the keys and half the values, into operands in LDS (32 KB at D = 128, two
 // steps' worth), while the codes of the next two steps are on their way in
 // registers; every wave multiplies the whole step with its own two tiles of 16
-// rows.  bf16 calls with many rows.  8 x 64 rows of 32 heads, contexts to 4352 (19.6 GFLOP): 46 us
-// a call, 38 of them this kernel.  A step takes a workgroup 1.4 us, of which the products are 0.85 at
-// the matrix cores' peak; the rest of the call is the first codes' way in, the parts of the
-// shares (28 MB out, and in again by the merge) and the longest context's shares.  Running the next
+// rows.  bf16 calls with many rows.  8 x 64 rows of 32 heads, contexts to 4352 (19.6 GFLOP): 47 us
+// a call; under a trace, which adds some, 43 this kernel and 8 the merge.  A step takes a workgroup 1.4 to 1.7 us, of which
+// the products are 0.85 at the matrix cores' peak, and the longest context's shares have 14: 20 to 24 us.  The
+// rest of the kernel is the first codes' way in, the parts of the shares (28 MB out, 5 us at the rate of a large copy) and the
+// workgroups that start late.  Running the next
 // step's first product under the exponentials (interleaved one to four instructions) measured the same.
 template <int D>
 struct KvqFromLds {
@@ -1102,8 +1104,14 @@ __global__ __launch_bounds__(256) void kvq_merge_kernel(KvqAttnArgs a) {
 // (1.0 at D = 64, 1.65 for 32 rows at D = 128) while the workgroups draw less than the HBM gives; rounds
 // in turn beyond about 200 workgroups (256: what the card holds of the widest), for contexts
 // are ragged and not all have their longest.  Waves that split the rows (256 or 128 a workgroup): a
-// round is 64 keys, 1.75 us while the workgroups fit the card, and 2 us for the start.  A second share
+// round is 64 keys, 1.75 us up to 340 workgroups of eight waves or 680 of four, and 2 us for the start.  A second share
 // adds the merge: its launch, and a part for each share.
+//
+// 340 and 680 are more than the card holds at D = 128 (256 and 512 at 220 and 236 registers): with ragged contexts some
+// shares are empty.  Requests of one length pay for that, since the workgroups past 256 then run after the others:
+// 8 of 4352, 64 tokens: 82 us (36 GFLOP; ragged 47, 20 GFLOP), 16 of 2064: 74 (34 GFLOP; ragged 66, 19 GFLOP).  D = 64 takes
+// the step of D = 128: it was not fitted (8 of 4352, 64 tokens: 36 us ragged, 59 of one length).  The causal triangle
+// of a prompt counts as its longest row too: 2048 tokens 70 us.
 //
 // Measured (us a call, 8B heads, contexts ragged up to the length; keys split, 128 and 256 rows
 // a workgroup): 8 requests of 1000, 64 tokens: 26, 33, 33; 8 of 4000, 33 tokens: 33, 43, 40; 8 of
@@ -1173,7 +1181,7 @@ void kvq_attention(KvqAttnArgs a, hipStream_t st) {
   a.part_s = (float2*)(a.part_o + kvq_part_rows(a) * a.D);
   // a negative scale turns the queries' signs
   a.neg = a.scale < 0.0;
-  // rows start on 16 bytes, heads then do (8 x 64 rows of 32 heads: 46 us, 51 by elements)
+  // rows start on 16 bytes, heads then do (8 x 64 rows of 32 heads: 47 us, 51 by elements)
   a.vec = (((uintptr_t)a.q | a.ld_q * (a.bf16 ? 2 : 4)) & 15) == 0;
   // a zero scale: the smallest number in its place, whose scores are below 2^-21 (0 * -inf is none where a key is hidden)
   a.scale_log2 = std::max(kvq_scale_log2(a.scale), 0x1p-149f);

@@ -17,7 +17,7 @@
 // in registers up to 32768 codes.
 //
 // Four rows of 16384 codes with top-k and top-p: 20.5 us a call, a chain of some fifteen
-// barriers in one workgroup each.  512 rows of 32768, settings of their own: 77 us (67 MB, 13 us
+// barriers in one workgroup each.  512 rows of 32768, settings of their own: 76 us (67 MB, 13 us
 // at the rate of a large copy; two rows a CU one after the other).  With the same settings in all rows:
 // reading and the draw 37, a top-k 21 more, a top-p 26, both 39: atomics on shared memory, one
 // or two a code at about a lane and cycle, and the float64 exponentials.  Rows that start on
@@ -155,7 +155,8 @@ struct LsRow {
       for (int i = 0; i < NG; ++i)
         if (i < groups) {
           // (values that the compiler takes for new ones: what a pass computes of them is computed in that
-          // pass, not ahead of the barriers before it nor kept from an earlier one, which ends in scratch memory)
+          // pass, not ahead of the barriers before it nor kept from an earlier one, which ends in scratch memory.  Of
+          // eight groups ten registers still do, 44 bytes a lane; of four none.)
           asm volatile("" : "+v"(held[i].x), "+v"(held[i].y), "+v"(held[i].z), "+v"(held[i].w));
           const float x[4] = {held[i].x, held[i].y, held[i].z, held[i].w};
           fn(beg + i * 256, x);
@@ -455,7 +456,7 @@ __global__ __launch_bounds__(LS_T) void sample_logits_kernel(SampleArgs a) {
   int bi = 0x7fffffff;
   const bool by_k = top_k > 0 && top_k < V, by_p = top_p < 1.0;
   if (by_k || by_p) {
-    const LsBins bins(fmaxf(floor_l, mn), mx);  // (from floor_l alone: 88 us in place of 75, warm rows share few bins)
+    const LsBins bins(fmaxf(floor_l, mn), mx);  // (from floor_l alone: 88 us in place of 76, warm rows share few bins)
     const LsCumul q = ls_histogram(row, wt, bins, by_k, by_p, 0u, 0ull, sh);
     double mass = 0.0;
     if (by_k) {
