@@ -613,7 +613,8 @@ struct KvqRows {
             if (neg) x = -x;
 #pragma unroll
             for (int pl = 0; pl < PL; ++pl) {  // (the last rounding of three takes what is left: 24 bits)
-              const uint16_t b = f2bf(x);
+              uint16_t b = f2bf(x);
+              if (pl == 0 && (b & 0x7FFF) == 0x7F80 && fabsf(x) < INFINITY) --b;  // rounded past the largest bf16: that one
               q[i][pl][kd][e] = __builtin_bit_cast(__bf16, b);
               x -= bf2f(b);
             }

@@ -10,7 +10,7 @@ import paper_2606_20543_amd as ssd
 import synth
 from tests import gpu_util as G
 from tests import serve_util as S
-from tests.test_gpu_serve_ops import Dev, cache_arrays, code, slot_case, typed, upload, values
+from tests.test_gpu_serve_ops import Dev, Raw, cache_arrays, code, slot_case, typed, upload, values
 
 pytestmark = pytest.mark.gpu
 
@@ -326,3 +326,22 @@ def test_an_error_of_an_earlier_call_is_not_this_ones(dev):
         hip.hipGetLastError()
         ssd.ssd_free_session(sess)
         pair.close()
+
+
+@pytest.mark.parametrize("width,hint", [(4, None), (90, 5000)])
+def test_attention_largest_queries(dev, width, hint):
+    """fp32 queries past the largest bf16 (255 2^120), keys small enough that scores stay ordinary: the three operands of a
+    query carry all of its bits."""
+    rng = np.random.default_rng(21)
+    heads, kv, D, block, L = 4, 2, 64, 64, 150
+    c, arrs, plain = cache_arrays(dev, rng, 4, kv, block, D)
+    upload(arrs[2], np.full((4, kv), 5, np.uint8))  # keys of some 2^-115
+    plain.ke[:] = 5
+    q = (rng.standard_normal((3, heads, D)) * 1e37).astype(np.float32)
+    top = np.finfo(np.float32).max
+    q[0, :, 3], q[1, :, 7], q[2, 0, 60] = top, -top, np.nextafter(np.float32(3.3953e38), np.float32(np.inf))
+    table = np.full((1, width), -1, np.int32)
+    table[0, :3] = [2, 0, 3]
+    got = attend(dev, c, "f32", q, [0, 3], [L], table, 2.0 ** -8, max_len=hint)
+    want, tol = S.attention(plain, q.astype(np.float64), [0, 3], [L], table, 2.0 ** -8, False)
+    assert float((np.abs(got - want) - tol).max()) <= 0
