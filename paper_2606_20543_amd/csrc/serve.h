@@ -347,7 +347,8 @@ __global__ __launch_bounds__(ROPE_T) void rope_axes_kernel(RopeArgs a, int TB) {
 }
 
 void rope_axes(const RopeArgs& a, hipStream_t st) {
-  const int TB = std::max(1, std::min(4, 1024 / a.half));
+  // tokens a workgroup: 12 KB of factors at most (fewer tokens would make 2^25 of them more threads than a launch takes)
+  const int TB = std::max(3, std::min(4, 1024 / a.half));
   const dim3 grid((a.T + TB - 1) / TB);
   const size_t lds = (size_t)TB * a.half * sizeof(float2);
   // 16-byte accesses where every row, head and half starts on one (the 16384 tokens above: 64 us, 150 by elements)

@@ -345,3 +345,30 @@ def test_attention_largest_queries(dev, width, hint):
     got = attend(dev, c, "f32", q, [0, 3], [L], table, 2.0 ** -8, max_len=hint)
     want, tol = S.attention(plain, q.astype(np.float64), [0, 3], [L], table, 2.0 ** -8, False)
     assert float((np.abs(got - want) - tol).max()) <= 0
+
+
+def test_rope_of_the_most_tokens(dev):
+    """2^25 - 1 tokens of heads of 684: the launch holds them (92 GB, in place); the first, the last and some rows between."""
+    T, D = 2 ** 25 - 1, 684
+    rng = np.random.default_rng(22)
+    x, val = typed(rng.standard_normal((2, 1, 1, D)), "bf16")
+    pos = np.zeros((1, T), np.int32)
+    at = [0, 1, 2, 3, 4, T // 2, T - 4, T - 3, T - 2, T - 1]
+    pos[0, at] = [0, 5, 17, 4000, 3, 99999, 12, 7, 2 ** 31 - 1, 1234]
+    p = ssd.ssd_rope_params(1, 1, D, ssd.SSD_BF16, 1, (D // 2,), D, D, D, D, 1e4)
+    dp, mem = dev(pos), []
+    try:
+        for side in x:
+            mem.append(Raw(T * D * 2))
+            for t in at:
+                mem[-1].put(t * D * 2, side)
+        ssd.ssd_rope_axes(p, T, mem[0].ptr, mem[1].ptr, dp.ptr, mem[0].ptr, mem[1].ptr)
+        for side, m in zip(val, mem):
+            for t in at:
+                want = S.rope(side, pos[:, t:t + 1], (D // 2,), 1e4)
+                got = S.bf16_value(m.get(t * D * 2, (1, 1, D), np.uint16)).astype(np.float64)
+                size = np.abs(side) + np.abs(np.roll(side, D // 2, -1))
+                assert (np.abs(got - want) <= size * (6 * 2.0 ** -24 + 2.0 ** 31 * 2.0 ** -50) + np.abs(want) * 2.0 ** -8).all(), t
+    finally:
+        for m in mem:
+            m.free()
